@@ -140,7 +140,7 @@ def prepare(case, seed):
     f32 = dict(dtype=torch.float32, device=DEV)
     s["out_logp"] = torch.zeros(M, **f32)
     if case["kind"] == "logp":
-        s["out_entropy"], s["out_lse"] = torch.zeros(M, n, **f32), torch.zeros(M, n, **f32)
+        s["out_entropy"], s["out_lse"] = torch.zeros(M, n, **f32), torch.zeros(M, n, 2, **f32)
         if case["grad"]:
             s["g_logp"], s["g_entropy"] = normal(M) / M, normal(M) * (0.01 / M)
     else:
@@ -176,7 +176,7 @@ def _by_type(s, logits):
 
 
 def _row_stats(s, inp):
-    """Joint log-probability, per-type entropy, per-type log-sum-exp, and the log-softmax's parts."""
+    """Joint log-probability, per-type entropy, per-type log-sum-exp (maximum, rest), and the log-softmax's parts."""
     z = _by_type(s, inp["logits"])
     top = z.amax(2, keepdim=True)
     top = torch.where(top == -math.inf, 0.0, top)
@@ -190,7 +190,8 @@ def _row_stats(s, inp):
     entropy = -(p * logs).sum(2)
     chosen = torch.gather(inp["logits"].double(), 1, inp["actions"].long())
     logp = torch.where(some[:, :, 0], chosen - lse[:, :, 0], 0.0).sum(1)
-    return logp, entropy, lse[:, :, 0], p, logs, some
+    parts = torch.stack([torch.where(some, top.double(), -math.inf), torch.where(some, torch.log(total), 0.0)], 3)
+    return logp, entropy, parts[:, :, 0], p, logs, some
 
 
 def _logit_grad(s, p, logs, entropy, some, g_logp, g_entropy):
@@ -298,7 +299,7 @@ def work(case):
     M, live, a, n = _rows(case), _live(case), case["a"], case["types"]
     es = 2 if case["dtype"] == "bf16" else 4
     grad = case["kind"] != "logp" or case["grad"]
-    per_row = {"logp": 4 * n + 4 + 8 * n + (8 + 8 * n if grad else 0), "loss": 4 * n + 20, "pref": 4 * n + 8}[case["kind"]]
+    per_row = {"logp": 4 * n + 4 + 12 * n + (8 + 12 * n if grad else 0), "loss": 4 * n + 20, "pref": 4 * n + 8}[case["kind"]]
     # maximum, difference, exponential, sum, entropy's product and sum; gradient: difference, exponential, product
     return {"bytes": es * a * (live + (M if grad else 0)) + per_row * M, "flops": a * live * (6 + (4 if grad else 0))}
 
@@ -312,7 +313,7 @@ def exact(case, seed):
     f64 = dict(dtype=torch.float64, device=DEV)
     pairs_of = list(zip(segs, segs[1:]))
     blocks = [slice(i, min(M, i + max(1, (1 << 26) // a))) for i in range(0, M, max(1, (1 << 26) // a))]
-    logp, H, L = torch.zeros(M, **f64), torch.zeros(M, len(pairs_of), **f64), torch.zeros(M, len(pairs_of), **f64)
+    logp, H, L, top = torch.zeros(M, **f64), *(torch.zeros(M, len(pairs_of), **f64) for _ in range(3))
     for b in blocks:
         z = s["logits"][b].double()
         for t, (lo, hi) in enumerate(pairs_of):
@@ -323,10 +324,11 @@ def exact(case, seed):
             none = torch.isinf(lse)
             logp[b] += torch.where(none, 0.0, chosen - lse)
             H[b, t], L[b, t] = torch.where(none, 0.0, -pl.nan_to_num(0.0).sum(1)), lse
+            top[b, t] = z[:, lo:hi].amax(1)
     one = lambda k: s[k].double()  # noqa: E731
     f = lambda v: float(torch.tensor(v, dtype=torch.float32))  # the calls take their parameters as fp32  # noqa: E731
     if case["kind"] == "logp":
-        out = dict(logp=logp, entropy=H, lse=L)
+        out = dict(logp=logp, entropy=H, lse=torch.stack([top, torch.where(torch.isinf(L), 0.0, L - top)], 2))
         if not case["grad"]:
             return out
         g, ge = one("g_logp"), one("g_entropy")
