@@ -17,8 +17,9 @@
  * Around the round: harl_track_advantage / harl_track_eliminate (reward, advantage and the
  * adaptive-stopping elimination of schedule tracks; Eq. 6, Section 5), harl_policy_select (one
  * action per modification type, greedy or sampled; Section 4.3), harl_ppo_update (the actor/critic's
- * training step; Section 6.1) and harl_gbdt_bin / harl_gbdt_round (the cost model's refit on
- * measured programs; Algorithm 1, Section 6.1).
+ * training step; Section 6.1), harl_policy_logp / harl_policy_loss / harl_preference_loss (the
+ * training objectives on the logits of any actor, with their gradients) and harl_gbdt_bin /
+ * harl_gbdt_round (the cost model's refit on measured programs; Algorithm 1, Section 6.1).
  *
  * Conventions for every call:
  *   - Return value is a harl_status; nothing else signals an error and no C++ exception crosses
@@ -298,6 +299,138 @@ int harl_ppo_update(const harl_ppo_config *cfg, float *d_params, float *d_adam_m
                     int32_t step, const float *d_states, const int32_t *d_actions,
                     const float *d_logp_old, const float *d_adv, const float *d_ret, int32_t M,
                     float *d_grad, float *d_loss, void *d_ws, size_t ws_bytes, void *stream);
+
+/* ============================================================================================
+ * Policy objectives on the logits of any actor: log-probabilities of chosen actions, the clipped
+ * policy loss with a KL term (Section 6.1: PPO, Schulman et al., 2017; the KL term to a reference
+ * policy as Schulman's non-negative estimator) and the pairwise preference loss of log ratios
+ * (Rafailov et al., NeurIPS'23), each with the gradient of the logits.  harl_ppo_update trains the
+ * library's own network; these calls are for an actor whose logits the caller computes, up to
+ * token heads as wide as a vocabulary.
+ * ============================================================================================ */
+
+#define HARL_HEAD_MAX_COLUMNS (1 << 20)      /* of a head of one segment                          */
+#define HARL_HEAD_MAX_TYPE_COLUMNS 4096      /* of a head of several segments                     */
+
+/* The logits rows of an actor: the element type of logits and gradient, a columns, and the
+ * segments (modification types) that a row is cut into, as in harl_policy_select.
+ * 1 <= n_seg <= HARL_SELECT_MAX_SEGMENTS; 1 <= a <= HARL_HEAD_MAX_COLUMNS, and with n_seg > 1
+ * a <= HARL_HEAD_MAX_TYPE_COLUMNS (HARL_E_UNSUPPORTED beyond). */
+typedef struct {
+    harl_dtype dtype;
+    int32_t a, n_seg;
+    int32_t seg_offsets[HARL_SELECT_MAX_SEGMENTS + 1];  /* 0 = o_0 < ... < o_n_seg = a */
+} harl_policy_head;
+
+/*
+ * Common to the calls below.
+ *   d_logits [M][ld] of head->dtype, aligned to its element (ld >= a; columns a .. ld-1 are not
+ *            read).  A logit of -inf is an excluded action: probability 0, gradient 0.  A segment of
+ *            nothing but -inf is empty: it adds 0 to log-probability and entropy and has gradient 0.
+ *            The log-probability of an excluded action in a segment that is not empty is -inf.  NaN
+ *            and +inf make their segment's results NaN.
+ *   d_actions [M][n_seg] int32: row-global indices, each in its segment; others are clamped into it.
+ *   Per row, over its segments s: lse_s = log sum exp(z), logp = sum_s (z[action_s] - lse_s),
+ *   H_s = -sum p log p.  The gradient of g_logp logp + g_H sum_s H_s at a logit is
+ *   g_logp (1[i = action] - p) - g_H p (log p + H_s).
+ *   d_dlogits [M][ld_d] of head->dtype out (rounded once, to nearest): the gradient; columns
+ *            a .. ld_d-1 are left as they were.  It may be d_logits itself with ld_d == ld (the
+ *            gradient replaces the logits); any other overlap is an error.
+ *   Sums are fp32 over a row's columns (a row's maximum subtracted) and fp64 over rows and segments.
+ *   16-byte alignment of the first row and of ld lets the kernels move 16 bytes at a time
+ *   throughout; other rows move 16 bytes at a time behind their first aligned column, and their
+ *   gradient does where d_dlogits has the same alignment.
+ * M >= 0 (M == 0 is a no-op).  Arrays other than logits and gradient are 4-byte aligned; d_ws is
+ * 256-byte aligned, its contents on entry do not matter.
+ */
+
+/* Bytes of device workspace harl_policy_logp needs for M rows. */
+size_t harl_policy_logp_workspace_size(const harl_policy_head *head, int32_t M);
+
+/*
+ * Log-probabilities and entropies of M rows (logp_old and logp_ref of the losses below).
+ *   d_logp    [M] fp32 out: the chosen actions' joint log-probability.
+ *   d_entropy [M][n_seg] fp32 out, or NULL: the segments' entropies.
+ *   d_lse     [M][n_seg][2] fp32 out, or NULL: the segments' log-sum-exp in two parts, the largest
+ *             logit m and log sum exp(z - m) ({-inf, 0} for an empty segment).  Apart they keep their
+ *             precision for logits of any size; their sum is the log-sum-exp.
+ */
+int harl_policy_logp(const harl_policy_head *head, const void *d_logits, int64_t ld, int32_t M,
+                     const int32_t *d_actions, float *d_logp, float *d_entropy, float *d_lse,
+                     void *d_ws, size_t ws_bytes, void *stream);
+
+/*
+ * Gradient of sum_r (d_g_logp[r] logp_r + d_g_entropy[r] sum_s H_rs) at the logits.
+ *   d_lse [M][n_seg][2], d_entropy [M][n_seg]: harl_policy_logp's outputs for the same logits;
+ *             d_entropy may be NULL where d_g_entropy is.
+ *   d_g_logp  [M] fp32; d_g_entropy [M] fp32 or NULL.
+ * Rows whose gradients are 0 are set to 0 and their logits are not read.
+ */
+int harl_policy_logp_grad(const harl_policy_head *head, const void *d_logits, int64_t ld, int32_t M,
+                          const int32_t *d_actions, const float *d_lse, const float *d_entropy,
+                          const float *d_g_logp, const float *d_g_entropy, void *d_dlogits,
+                          int64_t ld_d, void *stream);
+
+/* Hyper-parameters of harl_policy_loss: 0 <= clip_low < 1, clip_high >= 0, w_kl >= 0,
+ * w_entropy >= 0, all finite. */
+typedef struct {
+    float clip_low, clip_high;  /* the ratio is clipped to [1 - clip_low, 1 + clip_high] */
+    float w_kl, w_entropy;
+} harl_policy_loss_config;
+
+/* Bytes of device workspace harl_policy_loss needs for M rows. */
+size_t harl_policy_loss_workspace_size(const harl_policy_head *head, int32_t M);
+
+/*
+ * Clipped policy loss of M rows (transitions or tokens) and its gradient:
+ *   loss = sum_r w_r (-min(ratio A, clip(ratio) A) + w_kl (e^x - x - 1) - w_entropy sum_s H_s),
+ *   ratio = exp(logp - logp_old), x = logp_ref - logp;
+ * min passes the gradient to the unclipped term on equality, clip inside its closed range (as in
+ * harl_ppo_update, whose surrogate and entropy terms this gives for weights 1/M).
+ *   d_logp_old, d_adv [M] fp32; d_logp_ref [M] fp32, or NULL (no KL term; w_kl must be 0).
+ *   d_weight  [M] fp32, or NULL (1/M each).  A row of weight 0 is padding: none of its other values is
+ *             read, it adds nothing to any sum, its d_logp is 0 and its gradient row is 0.
+ *   d_dlogits out, or NULL; d_logp [M] fp32 out, or NULL.
+ *   d_loss    [4] fp32 out, or NULL: the loss, and the weighted sums of -min(..), of the KL term
+ *             without w_kl (0 without d_logp_ref) and of the entropies.
+ * An excluded action that was chosen has ratio 0 and an infinite KL term (NaN where logp_ref is
+ * -inf too).  Deterministic.
+ */
+int harl_policy_loss(const harl_policy_head *head, const harl_policy_loss_config *cfg,
+                     const void *d_logits, int64_t ld, int32_t M, const int32_t *d_actions,
+                     const float *d_logp_old, const float *d_logp_ref, const float *d_adv,
+                     const float *d_weight, void *d_dlogits, int64_t ld_d, float *d_logp,
+                     float *d_loss, void *d_ws, size_t ws_bytes, void *stream);
+
+/* Hyper-parameters of harl_preference_loss: beta > 0 finite, 0 <= smoothing < 1. */
+typedef struct {
+    float beta, smoothing;
+} harl_preference_config;
+
+/* Bytes of device workspace harl_preference_loss needs for n_rows rows in n_pairs pairs. */
+size_t harl_preference_loss_workspace_size(const harl_policy_head *head, int32_t n_rows, int32_t n_pairs);
+
+/*
+ * Preference loss of n_pairs pairs of tracks (sequences of rows) and its gradient.  Pair p prefers
+ * sequence 2p to sequence 2p + 1; sequence q owns rows [d_seq_ptr[q], d_seq_ptr[q+1]):
+ *   R_q = sum_r w_r (logp_r - logp_ref_r), h_p = beta (R_2p - R_2p+1),
+ *   loss = mean_p(-(1 - smoothing) log sigmoid(h_p) - smoothing log sigmoid(-h_p)).
+ *   d_logp_ref [n_rows] fp32, or NULL (zeros): the reference policy's log-probabilities.
+ *   d_weight   [n_rows] fp32, or NULL (ones).  A row of weight 0 (padding, a prompt) is treated as
+ *              in harl_policy_loss.
+ *   d_seq_ptr  [2 n_pairs + 1] int32, 0 <= d_seq_ptr[0] <= ... <= d_seq_ptr[2 n_pairs] <= n_rows
+ *              (caller's precondition; each bound is clamped to [0, n_rows]).  A sequence may be
+ *              empty (R = 0).  The gradient of rows before the first and behind the last sequence is left
+ *              as it was.
+ *   d_dlogits  out, or NULL; d_ratio [2 n_pairs] fp32 out, or NULL: R_q.
+ *   d_loss     [4] fp32 out, or NULL: the loss, and the means of -log sigmoid(h), of h and of [h > 0].
+ * n_pairs == 0 is a no-op; n_rows == 0 is not.  Deterministic.
+ */
+int harl_preference_loss(const harl_policy_head *head, const harl_preference_config *cfg,
+                         const void *d_logits, int64_t ld, int32_t n_rows, const int32_t *d_actions,
+                         const float *d_logp_ref, const float *d_weight, const int32_t *d_seq_ptr,
+                         int32_t n_pairs, void *d_dlogits, int64_t ld_d, float *d_ratio, float *d_loss,
+                         void *d_ws, size_t ws_bytes, void *stream);
 
 /* ============================================================================================
  * Schedule tracks between rounds: reward and advantage of a modification step (Algorithm 1,

@@ -258,6 +258,139 @@ int harl_ppo_update(const harl_ppo_config *cfg, float *d_params, float *d_adam_m
                                    M, d_grad, d_loss, d_ws, static_cast<hipStream_t>(stream));
 }
 
+static int head_check(const std::string &who, const harl_policy_head *h) {
+    if (!h) return fail(HARL_E_INVALID_ARG, who + ": null head");
+    if (h->dtype != HARL_F32 && h->dtype != HARL_BF16) return fail(HARL_E_INVALID_ARG, who + ": unknown dtype");
+    if (h->n_seg < 1 || h->n_seg > HARL_SELECT_MAX_SEGMENTS) return fail(HARL_E_INVALID_ARG, who + ": n_seg out of range");
+    if (h->a < 1) return fail(HARL_E_INVALID_ARG, who + ": need a >= 1");
+    if (h->a > HARL_HEAD_MAX_COLUMNS || (h->n_seg > 1 && h->a > HARL_HEAD_MAX_TYPE_COLUMNS))
+        return fail(HARL_E_UNSUPPORTED, who + ": too many columns");
+    if (h->seg_offsets[0] != 0 || h->seg_offsets[h->n_seg] != h->a)
+        return fail(HARL_E_INVALID_ARG, who + ": segments must run from 0 to a");
+    for (int s = 0; s < h->n_seg; ++s)
+        if (h->seg_offsets[s + 1] <= h->seg_offsets[s])
+            return fail(HARL_E_INVALID_ARG, who + ": segment offsets must increase");
+    return HARL_OK;
+}
+
+// Logits, actions and the optional gradient of M >= 1 rows.
+static int rows_check(const std::string &who, const harl_policy_head *h, const void *logits, int64_t ld, int32_t M,
+                      const int32_t *actions, const void *dlogits, int64_t ld_d) {
+    const size_t es = h->dtype == HARL_BF16 ? 2 : 4;
+    const int64_t most = ((int64_t)1 << 56) / M;
+    if (ld < h->a || ld > most) return fail(HARL_E_INVALID_ARG, who + ": need a <= ld (and rows that 2^56 elements hold)");
+    if (!logits || !aligned(logits, es)) return fail(HARL_E_INVALID_ARG, who + ": null or misaligned logits");
+    if (!actions || !aligned(actions, 4)) return fail(HARL_E_INVALID_ARG, who + ": null or misaligned actions");
+    if (!dlogits) return HARL_OK;
+    if (!aligned(dlogits, es)) return fail(HARL_E_INVALID_ARG, who + ": misaligned gradient");
+    if (ld_d < h->a || ld_d > most) return fail(HARL_E_INVALID_ARG, who + ": need a <= ld_d (and rows that 2^56 elements hold)");
+    if (dlogits == logits && ld_d == ld) return HARL_OK;
+    const uintptr_t z = reinterpret_cast<uintptr_t>(logits), d = reinterpret_cast<uintptr_t>(dlogits);
+    if (z < d + ((M - 1) * ld_d + h->a) * es && d < z + ((M - 1) * ld + h->a) * es)
+        return fail(HARL_E_INVALID_ARG, who + ": gradient and logits overlap without being the same rows");
+    return HARL_OK;
+}
+
+static int ws_check(const std::string &who, const void *ws, size_t ws_bytes, size_t need) {
+    if (!ws || !aligned(ws, 256)) return fail(HARL_E_INVALID_ARG, who + ": workspace null or not 256-byte aligned");
+    if (ws_bytes < need) return fail(HARL_E_WORKSPACE, who + ": workspace smaller than " + who + "_workspace_size()");
+    return HARL_OK;
+}
+
+size_t harl_policy_logp_workspace_size(const harl_policy_head *head, int32_t M) {
+    if (head_check("harl_policy_logp_workspace_size", head) != HARL_OK || M < 0) return 0;
+    return harl::objective_logp_ws_bytes(head, M);
+}
+
+int harl_policy_logp(const harl_policy_head *head, const void *d_logits, int64_t ld, int32_t M, const int32_t *d_actions,
+                     float *d_logp, float *d_entropy, float *d_lse, void *d_ws, size_t ws_bytes, void *stream) {
+    const char *who = "harl_policy_logp";
+    if (const int rc = head_check(who, head)) return rc;
+    if (M < 0) return fail(HARL_E_INVALID_ARG, "harl_policy_logp: negative size");
+    if (M == 0) return HARL_OK;
+    if (const int rc = rows_check(who, head, d_logits, ld, M, d_actions, nullptr, 0)) return rc;
+    if (!d_logp || !aligned(d_logp, 4) || (d_entropy && !aligned(d_entropy, 4)) || (d_lse && !aligned(d_lse, 4)))
+        return fail(HARL_E_INVALID_ARG, "harl_policy_logp: null or misaligned output");
+    if (const int rc = ws_check(who, d_ws, ws_bytes, harl::objective_logp_ws_bytes(head, M))) return rc;
+    return harl::policy_logp_launch(head, d_logits, ld, M, d_actions, d_logp, d_entropy, d_lse, d_ws,
+                                    static_cast<hipStream_t>(stream));
+}
+
+int harl_policy_logp_grad(const harl_policy_head *head, const void *d_logits, int64_t ld, int32_t M,
+                          const int32_t *d_actions, const float *d_lse, const float *d_entropy, const float *d_g_logp,
+                          const float *d_g_entropy, void *d_dlogits, int64_t ld_d, void *stream) {
+    const char *who = "harl_policy_logp_grad";
+    if (const int rc = head_check(who, head)) return rc;
+    if (M < 0) return fail(HARL_E_INVALID_ARG, "harl_policy_logp_grad: negative size");
+    if (M == 0) return HARL_OK;
+    if (!d_dlogits) return fail(HARL_E_INVALID_ARG, "harl_policy_logp_grad: null gradient");
+    if (const int rc = rows_check(who, head, d_logits, ld, M, d_actions, d_dlogits, ld_d)) return rc;
+    if (!d_lse || !aligned(d_lse, 4) || !d_g_logp || !aligned(d_g_logp, 4) || (d_entropy && !aligned(d_entropy, 4)) ||
+        (d_g_entropy && !aligned(d_g_entropy, 4)))
+        return fail(HARL_E_INVALID_ARG, "harl_policy_logp_grad: null or misaligned array");
+    if (d_g_entropy && !d_entropy) return fail(HARL_E_INVALID_ARG, "harl_policy_logp_grad: g_entropy needs the entropies");
+    return harl::policy_logp_grad_launch(head, d_logits, ld, M, d_actions, d_lse, d_entropy, d_g_logp, d_g_entropy,
+                                         d_dlogits, ld_d, static_cast<hipStream_t>(stream));
+}
+
+size_t harl_policy_loss_workspace_size(const harl_policy_head *head, int32_t M) {
+    if (head_check("harl_policy_loss_workspace_size", head) != HARL_OK || M < 0) return 0;
+    return harl::objective_loss_ws_bytes(head, M);
+}
+
+int harl_policy_loss(const harl_policy_head *head, const harl_policy_loss_config *cfg, const void *d_logits, int64_t ld,
+                     int32_t M, const int32_t *d_actions, const float *d_logp_old, const float *d_logp_ref,
+                     const float *d_adv, const float *d_weight, void *d_dlogits, int64_t ld_d, float *d_logp,
+                     float *d_loss, void *d_ws, size_t ws_bytes, void *stream) {
+    const char *who = "harl_policy_loss";
+    if (const int rc = head_check(who, head)) return rc;
+    if (!cfg || !(cfg->clip_low >= 0.f && cfg->clip_low < 1.f) || !(cfg->clip_high >= 0.f && cfg->clip_high < INFINITY) ||
+        !(cfg->w_kl >= 0.f && cfg->w_kl < INFINITY) || !(cfg->w_entropy >= 0.f && cfg->w_entropy < INFINITY))
+        return fail(HARL_E_INVALID_ARG, "harl_policy_loss: null config or hyper-parameter out of range");
+    if (M < 0) return fail(HARL_E_INVALID_ARG, "harl_policy_loss: negative size");
+    if (M == 0) return HARL_OK;
+    if (const int rc = rows_check(who, head, d_logits, ld, M, d_actions, d_dlogits, ld_d)) return rc;
+    if (!d_logp_old || !aligned(d_logp_old, 4) || !d_adv || !aligned(d_adv, 4) || (d_logp_ref && !aligned(d_logp_ref, 4)) ||
+        (d_weight && !aligned(d_weight, 4)))
+        return fail(HARL_E_INVALID_ARG, "harl_policy_loss: null or misaligned array");
+    if (cfg->w_kl != 0.f && !d_logp_ref) return fail(HARL_E_INVALID_ARG, "harl_policy_loss: w_kl needs logp_ref");
+    if ((d_logp && !aligned(d_logp, 4)) || (d_loss && !aligned(d_loss, 4)))
+        return fail(HARL_E_INVALID_ARG, "harl_policy_loss: misaligned output");
+    if (const int rc = ws_check(who, d_ws, ws_bytes, harl::objective_loss_ws_bytes(head, M))) return rc;
+    return harl::policy_loss_launch(head, cfg, d_logits, ld, M, d_actions, d_logp_old, d_logp_ref, d_adv, d_weight,
+                                    d_dlogits, ld_d, d_logp, d_loss, d_ws, static_cast<hipStream_t>(stream));
+}
+
+size_t harl_preference_loss_workspace_size(const harl_policy_head *head, int32_t n_rows, int32_t n_pairs) {
+    if (head_check("harl_preference_loss_workspace_size", head) != HARL_OK || n_rows < 0 || n_pairs < 0 ||
+        n_pairs > (1 << 30) - 1)
+        return 0;
+    return harl::objective_preference_ws_bytes(head, n_rows, n_pairs);
+}
+
+int harl_preference_loss(const harl_policy_head *head, const harl_preference_config *cfg, const void *d_logits, int64_t ld,
+                         int32_t n_rows, const int32_t *d_actions, const float *d_logp_ref, const float *d_weight,
+                         const int32_t *d_seq_ptr, int32_t n_pairs, void *d_dlogits, int64_t ld_d, float *d_ratio,
+                         float *d_loss, void *d_ws, size_t ws_bytes, void *stream) {
+    const char *who = "harl_preference_loss";
+    if (const int rc = head_check(who, head)) return rc;
+    if (!cfg || !(cfg->beta > 0.f && cfg->beta < INFINITY) || !(cfg->smoothing >= 0.f && cfg->smoothing < 1.f))
+        return fail(HARL_E_INVALID_ARG, "harl_preference_loss: null config or hyper-parameter out of range");
+    if (n_rows < 0 || n_pairs < 0 || n_pairs > (1 << 30) - 1)
+        return fail(HARL_E_INVALID_ARG, "harl_preference_loss: size out of range");
+    if (n_pairs == 0) return HARL_OK;
+    if (n_rows > 0)
+        if (const int rc = rows_check(who, head, d_logits, ld, n_rows, d_actions, d_dlogits, ld_d)) return rc;
+    if ((d_logp_ref && !aligned(d_logp_ref, 4)) || (d_weight && !aligned(d_weight, 4)) || !d_seq_ptr || !aligned(d_seq_ptr, 4))
+        return fail(HARL_E_INVALID_ARG, "harl_preference_loss: null or misaligned array");
+    if ((d_ratio && !aligned(d_ratio, 4)) || (d_loss && !aligned(d_loss, 4)))
+        return fail(HARL_E_INVALID_ARG, "harl_preference_loss: misaligned output");
+    if (const int rc = ws_check(who, d_ws, ws_bytes, harl::objective_preference_ws_bytes(head, n_rows, n_pairs))) return rc;
+    return harl::preference_loss_launch(head, cfg, d_logits, ld, n_rows, d_actions, d_logp_ref, d_weight, d_seq_ptr,
+                                        n_pairs, d_dlogits, ld_d, d_ratio, d_loss, d_ws,
+                                        static_cast<hipStream_t>(stream));
+}
+
 int harl_track_advantage(const float *d_c_prev, const float *d_c_next, const float *d_v_prev, const float *d_v_next,
                          int32_t n, float gamma, float eps, float *d_reward, float *d_adv, void *stream) {
     if (n < 0) return fail(HARL_E_INVALID_ARG, "harl_track_advantage: negative size");

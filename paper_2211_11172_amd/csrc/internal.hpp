@@ -134,6 +134,23 @@ int ppo_update_launch(const harl_ppo_config *c, float *params, float *adam_m, fl
 int policy_select_launch(const float *logits, int32_t B, int32_t a, const int32_t *seg_offsets, int32_t n_seg,
                          uint32_t flags, uint64_t seed, uint64_t counter, int32_t *action, float *logp, float *probs,
                          hipStream_t stream);
+// policy objectives (objective.hip)
+size_t objective_logp_ws_bytes(const harl_policy_head *head, int32_t M);
+int policy_logp_launch(const harl_policy_head *head, const void *logits, int64_t ld, int32_t M, const int32_t *actions,
+                       float *logp, float *entropy, float *lse, void *ws, hipStream_t stream);
+int policy_logp_grad_launch(const harl_policy_head *head, const void *logits, int64_t ld, int32_t M,
+                            const int32_t *actions, const float *lse, const float *entropy, const float *g_logp,
+                            const float *g_entropy, void *dlogits, int64_t ld_d, hipStream_t stream);
+size_t objective_loss_ws_bytes(const harl_policy_head *head, int32_t M);
+int policy_loss_launch(const harl_policy_head *head, const harl_policy_loss_config *cfg, const void *logits, int64_t ld,
+                       int32_t M, const int32_t *actions, const float *logp_old, const float *logp_ref,
+                       const float *adv, const float *weight, void *dlogits, int64_t ld_d, float *logp, float *loss,
+                       void *ws, hipStream_t stream);
+size_t objective_preference_ws_bytes(const harl_policy_head *head, int32_t n_rows, int32_t n_pairs);
+int preference_loss_launch(const harl_policy_head *head, const harl_preference_config *cfg, const void *logits,
+                           int64_t ld, int32_t n_rows, const int32_t *actions, const float *logp_ref,
+                           const float *weight, const int32_t *seq_ptr, int32_t n_pairs, void *dlogits, int64_t ld_d,
+                           float *ratio, float *loss, void *ws, hipStream_t stream);
 int track_eliminate_launch(const float *adv, int32_t n, int32_t n_keep, int32_t *keep_index, const void *rows,
                            int64_t row_bytes, void *rows_out, void *ws, hipStream_t stream);
 

@@ -22,6 +22,8 @@ HARL_TOPK_MAX_K = 2048
 HARL_TOPK_MERGE = 1
 HARL_SELECT_MAX_SEGMENTS = 32
 HARL_SELECT_SAMPLE = 1
+HARL_HEAD_MAX_COLUMNS = 1 << 20
+HARL_HEAD_MAX_TYPE_COLUMNS = 4096
 
 # every entry point declared in include/harl.h
 EXPORTS = (
@@ -32,6 +34,9 @@ EXPORTS = (
     "harl_topk_workspace_size", "harl_topk", "harl_topk_reset", "harl_topk_static",
     "harl_policy_select",
     "harl_ppo_param_count", "harl_ppo_workspace_size", "harl_ppo_update",
+    "harl_policy_logp_workspace_size", "harl_policy_logp", "harl_policy_logp_grad",
+    "harl_policy_loss_workspace_size", "harl_policy_loss",
+    "harl_preference_loss_workspace_size", "harl_preference_loss",
     "harl_track_advantage", "harl_track_keep_count", "harl_track_eliminate_workspace_size", "harl_track_eliminate",
     "harl_gbdt_bin", "harl_gbdt_round_workspace_size", "harl_gbdt_round",
 )
@@ -57,6 +62,40 @@ def ppo_config(s: int, h1: int, h2: int, a: int, segs, clip_eps=0.2, w_value=0.5
     c.clip_eps, c.w_value, c.w_entropy = clip_eps, w_value, w_entropy
     c.lr_actor, c.lr_critic, c.beta1, c.beta2, c.adam_eps = lr_actor, lr_critic, beta1, beta2, adam_eps
     return c
+
+
+class PolicyHead(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("a", ctypes.c_int32), ("n_seg", ctypes.c_int32),
+                ("seg_offsets", ctypes.c_int32 * (HARL_SELECT_MAX_SEGMENTS + 1))]
+
+
+def policy_head(dtype: str, a: int, segs=None) -> PolicyHead:
+    """The logits rows of an actor: dtype "f32" or "bf16", a columns, segments segs (0 .. a; default one)."""
+    segs = (0, a) if segs is None else segs
+    if len(segs) - 1 > HARL_SELECT_MAX_SEGMENTS:
+        raise ValueError("policy_head: more than %d segments" % HARL_SELECT_MAX_SEGMENTS)
+    h = PolicyHead()
+    h.dtype, h.a, h.n_seg = {"f32": HARL_F32, "bf16": HARL_BF16}[dtype], a, len(segs) - 1
+    for i, o in enumerate(segs):
+        h.seg_offsets[i] = int(o)
+    return h
+
+
+class PolicyLossConfig(ctypes.Structure):
+    _fields_ = [("clip_low", ctypes.c_float), ("clip_high", ctypes.c_float), ("w_kl", ctypes.c_float),
+                ("w_entropy", ctypes.c_float)]
+
+
+def policy_loss_config(clip_low=0.2, clip_high=0.2, w_kl=0.0, w_entropy=0.0) -> PolicyLossConfig:
+    return PolicyLossConfig(clip_low, clip_high, w_kl, w_entropy)
+
+
+class PreferenceConfig(ctypes.Structure):
+    _fields_ = [("beta", ctypes.c_float), ("smoothing", ctypes.c_float)]
+
+
+def preference_config(beta=0.1, smoothing=0.0) -> PreferenceConfig:
+    return PreferenceConfig(beta, smoothing)
 
 
 class GbdtParams(ctypes.Structure):
@@ -127,6 +166,13 @@ def load():
                 "harl_ppo_update": ([P, P, P, P, i32, P, P, P, P, P, i32, P, P, P, sz, P], ctypes.c_int),
                 "harl_policy_select": ([P, i32, i32, P, i32, u32, ctypes.c_uint64, ctypes.c_uint64, P, P, P, P],
                                        ctypes.c_int),
+                "harl_policy_logp_workspace_size": ([P, i32], sz),
+                "harl_policy_logp": ([P, P, i64, i32, P, P, P, P, P, sz, P], ctypes.c_int),
+                "harl_policy_logp_grad": ([P, P, i64, i32, P, P, P, P, P, P, i64, P], ctypes.c_int),
+                "harl_policy_loss_workspace_size": ([P, i32], sz),
+                "harl_policy_loss": ([P, P, P, i64, i32, P, P, P, P, P, P, i64, P, P, P, sz, P], ctypes.c_int),
+                "harl_preference_loss_workspace_size": ([P, i32, i32], sz),
+                "harl_preference_loss": ([P, P, P, i64, i32, P, P, P, P, i32, P, i64, P, P, P, sz, P], ctypes.c_int),
                 "harl_track_advantage": ([P, P, P, P, i32, ctypes.c_float, ctypes.c_float, P, P, P], ctypes.c_int),
                 "harl_track_keep_count": ([i32, ctypes.c_double, P], ctypes.c_int),
                 "harl_track_eliminate_workspace_size": ([i32], sz),
@@ -308,6 +354,52 @@ def harl_ppo_update(cfg: PpoConfig, params, adam_m, adam_v, step: int, states, a
     _check(load().harl_ppo_update(ctypes.byref(cfg), _ptr(params), _ptr(adam_m), _ptr(adam_v), step, _ptr(states),
                                   _ptr(actions), _ptr(logp_old), _ptr(adv), _ptr(ret), M, _ptr(grad), _ptr(loss),
                                   _ptr(ws), ws_bytes, _stream(stream)), "harl_ppo_update")
+
+
+# ------------------------------------------------------------------------------------------------
+# policy objectives on the logits of any actor
+# ------------------------------------------------------------------------------------------------
+def harl_policy_logp_workspace_size(head: PolicyHead, M: int) -> int:
+    return int(load().harl_policy_logp_workspace_size(ctypes.byref(head), M))
+
+
+def harl_policy_logp(head: PolicyHead, logits, ld: int, M: int, actions, logp, entropy=None, lse=None, ws=None,
+                     ws_bytes: int = 0, stream=None):
+    _check(load().harl_policy_logp(ctypes.byref(head), _ptr(logits), ld, M, _ptr(actions), _ptr(logp), _ptr(entropy),
+                                   _ptr(lse), _ptr(ws), ws_bytes, _stream(stream)), "harl_policy_logp")
+
+
+def harl_policy_logp_grad(head: PolicyHead, logits, ld: int, M: int, actions, lse, entropy, g_logp, g_entropy, dlogits,
+                          ld_d: int, stream=None):
+    _check(load().harl_policy_logp_grad(ctypes.byref(head), _ptr(logits), ld, M, _ptr(actions), _ptr(lse),
+                                        _ptr(entropy), _ptr(g_logp), _ptr(g_entropy), _ptr(dlogits), ld_d,
+                                        _stream(stream)), "harl_policy_logp_grad")
+
+
+def harl_policy_loss_workspace_size(head: PolicyHead, M: int) -> int:
+    return int(load().harl_policy_loss_workspace_size(ctypes.byref(head), M))
+
+
+def harl_policy_loss(head: PolicyHead, cfg: PolicyLossConfig, logits, ld: int, M: int, actions, logp_old, logp_ref, adv,
+                     weight=None, dlogits=None, ld_d: int = 0, logp=None, loss=None, ws=None, ws_bytes: int = 0,
+                     stream=None):
+    _check(load().harl_policy_loss(ctypes.byref(head), ctypes.byref(cfg), _ptr(logits), ld, M, _ptr(actions),
+                                   _ptr(logp_old), _ptr(logp_ref), _ptr(adv), _ptr(weight), _ptr(dlogits), ld_d,
+                                   _ptr(logp), _ptr(loss), _ptr(ws), ws_bytes, _stream(stream)), "harl_policy_loss")
+
+
+def harl_preference_loss_workspace_size(head: PolicyHead, n_rows: int, n_pairs: int) -> int:
+    return int(load().harl_preference_loss_workspace_size(ctypes.byref(head), n_rows, n_pairs))
+
+
+def harl_preference_loss(head: PolicyHead, cfg: PreferenceConfig, logits, ld: int, n_rows: int, actions, logp_ref,
+                         weight, seq_ptr, n_pairs: int, dlogits=None, ld_d: int = 0, ratio=None, loss=None, ws=None,
+                         ws_bytes: int = 0, stream=None):
+    """seq_ptr: device int32 [2 n_pairs + 1]; sequence 2p is preferred to sequence 2p + 1."""
+    _check(load().harl_preference_loss(ctypes.byref(head), ctypes.byref(cfg), _ptr(logits), ld, n_rows, _ptr(actions),
+                                       _ptr(logp_ref), _ptr(weight), _ptr(seq_ptr), n_pairs, _ptr(dlogits), ld_d,
+                                       _ptr(ratio), _ptr(loss), _ptr(ws), ws_bytes, _stream(stream)),
+           "harl_preference_loss")
 
 
 # ------------------------------------------------------------------------------------------------
