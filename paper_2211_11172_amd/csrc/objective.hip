@@ -204,27 +204,440 @@ __device__ __forceinline__ void sum_terms(const double *__restrict__ terms, int6
     for (int c = 0; c < N; ++c) out[c] = part[c][0];
 }
 
+__device__ __forceinline__ void write_loss(const double (&s)[3], float w_kl, float w_entropy, float *loss) {
+    loss[0] = (float)(s[0] + (w_kl != 0.f ? (double)w_kl * s[1] : 0.0) - (w_entropy != 0.f ? (double)w_entropy * s[2] : 0.0));
+    for (int c = 0; c < 3; ++c) loss[1 + c] = (float)s[c];
+}
+
 __global__ __launch_bounds__(kThreads) void k_loss_sum(const double *__restrict__ terms, int64_t n, float w_kl,
                                                        float w_entropy, float *__restrict__ loss) {
     double s[3];
     sum_terms<3>(terms, n, s);
-    if (threadIdx.x == 0) {
-        loss[0] = (float)(s[0] + (w_kl != 0.f ? (double)w_kl * s[1] : 0.0) - (w_entropy != 0.f ? (double)w_entropy * s[2] : 0.0));
-        for (int c = 0; c < 3; ++c) loss[1 + c] = (float)s[c];
+    if (threadIdx.x == 0) write_loss(s, w_kl, w_entropy, loss);
+}
+
+// ------------------------------------------------------------------------------------------------
+// Heads of one segment.  A row is moved as 16-byte vectors behind its first aligned column; the columns
+// before it and behind the last whole vector (at most 2 (16 / element - 1)) are an element a thread.
+//
+// The exponentials are 2^y, y = (z - m) log2 e, with s = sum 2^y and u = sum 2^y y, so that
+//   log s = ln 2 log2 s,  H = ln 2 (log2 s - u / s).
+// log2 e is rounded to fp32 once for all columns: 2^y is e^(z - m) to the power 1 - 1.3e-8, which moves log s
+// by 1.3e-8 ln 2 u / s (6e-8 for a vocabulary's logits, the same sign in every row of a track); log_sum
+// adds it back.
+// ------------------------------------------------------------------------------------------------
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr double kLn2d = 0.69314718055994530942, kLog2eRest = 1.44269504088896340736 - (double)kLog2e;
+constexpr float kYMin = -160.f;  // 2^y is 0 from here on; keeps 0 times y a number for excluded actions
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ float exp2_hw(float y) { return __builtin_amdgcn_exp2f(y); }
+__device__ __forceinline__ float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
+template <typename T>
+constexpr int kVec = 16 / (int)sizeof(T);
+
+__device__ __forceinline__ void unpack(const uint4 &r, float (&x)[4]) {
+    x[0] = __uint_as_float(r.x);
+    x[1] = __uint_as_float(r.y);
+    x[2] = __uint_as_float(r.z);
+    x[3] = __uint_as_float(r.w);
+}
+__device__ __forceinline__ void unpack(const uint4 &r, float (&x)[8]) {
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(w[i] << 16);
+        x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
     }
 }
+__device__ __forceinline__ uint4 pack(const float (&x)[4]) {
+    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+}
+__device__ __forceinline__ uint4 pack(const float (&x)[8]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){x[2 * i], x[2 * i + 1]}, bf16x2));
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <typename T>
+__device__ __forceinline__ uint4 all_excluded() {
+    constexpr uint32_t w = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;
+    return make_uint4(w, w, w, w);
+}
+
+// The parts of a row: `head` columns, `full` vectors, `tail` columns.
+template <typename T>
+struct Parts {
+    int head, full, tail;
+    __device__ __forceinline__ Parts(const T *p, int a) {
+        const int mis = (int)(reinterpret_cast<uintptr_t>(p) / sizeof(T)) & (kVec<T> - 1);
+        head = mis ? min(kVec<T> - mis, a) : 0;
+        full = (a - head) / kVec<T>;
+        tail = a - head - full * kVec<T>;
+    }
+    // the column of thread t's single element, or -1
+    __device__ __forceinline__ int edge(int t) const {
+        return t < head ? t : t < head + tail ? full * kVec<T> + t : -1;
+    }
+};
+
+// Running sums of one lane, wave or workgroup relative to its own largest value.
+struct Sums {
+    float m, s, u;
+};
+
+__device__ __forceinline__ float shift_of(float m) { return m == -INFINITY ? 0.f : m; }
+
+// Moves the sums to a larger maximum (its shift ms = shift_of(m_new)).
+__device__ __forceinline__ void rescale(Sums &q, float m_new, float ms) {
+    const float d = (q.m - ms) * kLog2e, f = exp2_hw(d);
+    q.u = f * (q.u + q.s * fmaxf(d, -1e4f));
+    q.s *= f;
+    q.m = m_new;
+}
+
+template <int N>
+__device__ __forceinline__ void add_values(Sums &q, const float (&x)[N]) {
+    float gm = x[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) gm = max_nan(gm, x[i]);
+    const float m = max_nan(q.m, gm), ms = shift_of(m);
+    rescale(q, m, ms);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float y = fmaxf((x[i] - ms) * kLog2e, kYMin), e = exp2_hw(y);
+        q.s += e;
+        q.u = fmaf(e, y, q.u);
+    }
+}
+
+// Reductions over the first W lanes of a wave (W a power of two up to 64); the result in every lane.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float dpp(float x, float old) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(old), __float_as_int(x), CTRL, ROWS, 0xf, false));
+}
+template <int W, typename Op>
+__device__ __forceinline__ float lanes_reduce(float x, float none, Op op) {
+    if constexpr (W > 1) x = op(x, dpp<0x111, 0xf>(x, none));   // row_shr:1
+    if constexpr (W > 2) x = op(x, dpp<0x112, 0xf>(x, none));   // row_shr:2
+    if constexpr (W > 4) x = op(x, dpp<0x114, 0xf>(x, none));   // row_shr:4
+    if constexpr (W > 8) x = op(x, dpp<0x118, 0xf>(x, none));   // row_shr:8
+    if constexpr (W > 16) x = op(x, dpp<0x142, 0xa>(x, none));  // row_bcast:15 into rows 1 and 3
+    if constexpr (W > 32) x = op(x, dpp<0x143, 0xc>(x, none));  // row_bcast:31 into rows 2 and 3
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), W - 1));
+}
+template <int W>
+__device__ __forceinline__ Sums lanes_join(Sums q) {
+    const float m = lanes_reduce<W>(q.m, -INFINITY, [](float a, float b) { return max_nan(a, b); });
+    rescale(q, m, shift_of(m));
+    const auto add = [](float a, float b) { return a + b; };
+    return Sums{m, lanes_reduce<W>(q.s, 0.f, add), lanes_reduce<W>(q.u, 0.f, add)};
+}
+
+// The sums of a row from those of its TPR threads, in every thread.  `red` has 2 halves of TPR / 64
+// entries, used in turn, so that one barrier a row is enough.
+template <int TPR>
+__device__ __forceinline__ Sums row_join(Sums q, Sums (*red)[16], int &half) {
+    q = lanes_join<64>(q);
+    if constexpr (TPR > 64) {
+        constexpr int W = TPR / 64;
+        if (threadIdx.x % 64 == 0) red[half][threadIdx.x / 64] = q;
+        __syncthreads();
+        q = lanes_join<W>(red[half][threadIdx.x % W]);
+        half ^= 1;
+    }
+    // NaN or +inf among the values: everything that follows is NaN
+    if (!(q.m < INFINITY)) q.s = q.u = __builtin_nanf("");
+    return q;
+}
+
+__device__ __forceinline__ double log_sum(const Sums &q) {
+    return log((double)q.s) + kLog2eRest * kLn2d * kLn2d * (double)q.u / (double)q.s;
+}
+__device__ __forceinline__ double log_prob(const Sums &q, float zact) {
+    return q.s == 0.f ? 0.0 : ((double)zact - (double)q.m) - log_sum(q);
+}
+__device__ __forceinline__ double entropy_of(const Sums &q) {
+    return q.s == 0.f ? 0.0 : log_sum(q) - kLn2d * (double)q.u / (double)q.s;
+}
+
+// What the gradient of a row is made of: dz_i = -p_i (g + h (y_i + shift of H)) and g more at the action,
+// p = 2^y, y = (z - m) log2 e - log2 s.  Written as p (c + e y): c = -(g_logp + g_H H), e = -g_H ln 2.
+struct RowCoef {
+    float m, l2s, c, e, g, zero;  // zero != 0: the row's gradient is 0
+};
+
+__device__ __forceinline__ RowCoef coef_of(float m, float s, float l2s, float H, float gl, float ge) {
+    RowCoef k;
+    k.m = shift_of(m);
+    k.l2s = l2s;
+    k.c = -(gl + (ge != 0.f ? ge * H : 0.f));
+    k.e = -ge * kLn2;
+    k.g = gl;
+    k.zero = s == 0.f || (gl == 0.f && ge == 0.f) ? 1.f : 0.f;
+    return k;
+}
+
+template <bool ENT>
+__device__ __forceinline__ float grad_of(const RowCoef &k, float z) {
+    float y = fmaf(z - k.m, kLog2e, -k.l2s);
+    if constexpr (ENT) {
+        const float p = exp2_hw(y);
+        return p * fmaf(k.e, fmaxf(y, kYMin), k.c);
+    }
+    return exp2_hw(y) * k.c;
+}
+__device__ __forceinline__ float grad_any(const RowCoef &k, float z) {
+    return k.e != 0.f ? grad_of<true>(k, z) : grad_of<false>(k, z);
+}
+
+// One vector's gradient to column i0 of the row dz; `same`: dz has the logits' alignment.
+template <typename T>
+__device__ __forceinline__ void store_vec(T *dz, int i0, const float (&x)[kVec<T>], bool same) {
+    if (same) {
+        *reinterpret_cast<uint4 *>(dz + i0) = pack(x);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kVec<T>; ++i) store(dz + i0 + i, x[i]);
+    }
+}
+template <typename T>
+__device__ __forceinline__ void grad_vec(T *dz, int i0, const uint4 &raw, const RowCoef &k, bool same) {
+    float x[kVec<T>];
+    unpack(raw, x);
+    if (k.zero != 0.f) {
+#pragma unroll
+        for (int i = 0; i < kVec<T>; ++i) x[i] = 0.f;
+    } else if (k.e != 0.f) {
+#pragma unroll
+        for (int i = 0; i < kVec<T>; ++i) x[i] = grad_of<true>(k, x[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kVec<T>; ++i) x[i] = grad_of<false>(k, x[i]);
+    }
+    store_vec<T>(dz, i0, x, same);
+}
+
+// ---- statistics of (row, chunk) items: a chunk is `per` vectors, the first also has the row's edges ----
+enum Out : int { kPartial = 0, kLogp = 1 };
+
+struct StatOut {
+    Stat *stat;  // kPartial: [row][chunk] {m, s, u, z[action]}
+    float *logp, *entropy, *lse;
+};
+
+template <typename T, int TPR, int NV, int OUT>
+__global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void k_stats(Rows q, int chunks, int per, StatOut o) {
+    constexpr int WG = TPR < kThreads ? kThreads : TPR, N = kVec<T>;
+    __shared__ Sums red[2][16];
+    int half = 0;
+    const int t = threadIdx.x % TPR;
+    const int64_t items = (int64_t)q.M * chunks;
+    for (int64_t it = (int64_t)blockIdx.x * (WG / TPR) + threadIdx.x / TPR; it < items; it += (int64_t)gridDim.x * (WG / TPR)) {
+        const int r = chunks == 1 ? (int)it : (int)((uint32_t)it / (uint32_t)chunks), c = (int)(it - (int64_t)r * chunks);
+        if (!row_counts(q, r)) continue;
+        const T *z = static_cast<const T *>(q.z) + (int64_t)r * q.ld;
+        const Parts<T> parts(z, q.a);
+        const int act = min(max(q.act[r], 0), q.a - 1);
+        const float zact = to_f32(z[act]);
+        Sums sum{-INFINITY, 0.f, 0.f};
+        const int v1 = min((c + 1) * per, parts.full);
+        const T *body = z + parts.head;
+        for (int v = c * per + t; v < v1; v += TPR * NV) {
+            uint4 raw[NV];
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+                raw[j] = v + TPR * j < v1 ? *reinterpret_cast<const uint4 *>(body + (int64_t)(v + TPR * j) * N) : all_excluded<T>();
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                float x[N];
+                unpack(raw[j], x);
+                add_values<N>(sum, x);
+            }
+        }
+        if (c == 0 && parts.head + parts.tail > 0) {
+            const int i = parts.edge(t);
+            const float x[1] = {i < 0 ? -INFINITY : to_f32(z[i])};
+            add_values<1>(sum, x);
+        }
+        sum = row_join<TPR>(sum, red, half);
+        if (t == 0) {
+            if (OUT == kPartial) {
+                o.stat[it] = Stat{sum.m, sum.s, sum.u, zact};
+            } else {
+                o.logp[r] = (float)log_prob(sum, zact);
+                if (o.entropy) o.entropy[r] = (float)entropy_of(sum);
+                if (o.lse) {
+                    o.lse[2 * (int64_t)r] = sum.m;
+                    o.lse[2 * (int64_t)r + 1] = sum.s == 0.f ? 0.f : (float)log_sum(sum);
+                }
+            }
+        }
+    }
+}
+
+// A row's sums from its chunks', by one thread in chunk order.
+__device__ __forceinline__ Sums join_chunks(const Stat *st, int chunks) {
+    Sums q{st[0].m, st[0].s, st[0].u};
+    if (chunks == 1) return q;
+    for (int c = 1; c < chunks; ++c) q.m = max_nan(q.m, st[c].m);
+    const float m = q.m, ms = shift_of(m);
+    q = Sums{m, 0.f, 0.f};
+    for (int c = 0; c < chunks; ++c) {
+        Sums x{st[c].m, st[c].s, st[c].u};
+        rescale(x, m, ms);
+        q.s += x.s;
+        q.u += x.u;
+    }
+    if (!(m < INFINITY)) q.s = q.u = __builtin_nanf("");
+    return q;
+}
+
+__global__ __launch_bounds__(64) void k_logp_join(const Stat *__restrict__ stat, int M, int chunks, StatOut o) {
+    for (int64_t r = (int64_t)blockIdx.x * 64 + threadIdx.x; r < M; r += (int64_t)gridDim.x * 64) {
+        const Sums sum = join_chunks(stat + r * chunks, chunks);
+        o.logp[r] = (float)log_prob(sum, stat[r * chunks].zact);
+        if (o.entropy) o.entropy[r] = (float)entropy_of(sum);
+        if (o.lse) {
+            o.lse[2 * r] = sum.m;
+            o.lse[2 * r + 1] = sum.s == 0.f ? 0.f : (float)log_sum(sum);
+        }
+    }
+}
+
+// ---- the clipped loss, a row's logits held in registers between its sums and its gradient ----
+struct LossOut {
+    void *dz;
+    int64_t ld_d;
+    float *logp;
+    double *terms;  // [workgroup][3]: the sums of its rows' terms, in row order
+};
+
+// loss_row in fp32: every wave of a row evaluates this.
+__device__ __forceinline__ void loss_grad(const LossArgs &a, float w, float old, float ref, float adv, float logp, float &gl, float &ge) {
+    const float ratio = exp2_hw((logp - old) * kLog2e);
+    const float lo = 1.f - a.clip_low, hi = 1.f + a.clip_high;
+    const float s1 = ratio * adv, s2 = (ratio < lo ? lo : ratio > hi ? hi : ratio) * adv;
+    const bool inside = ratio >= lo && ratio <= hi;
+    const float ds = s2 < s1 && !inside ? 0.f : -s1;
+    const float dk = a.w_kl != 0.f ? a.w_kl * (1.f - exp2_hw((ref - logp) * kLog2e)) : 0.f;
+    gl = w * (ds + dk);
+    ge = -w * a.w_entropy;
+}
+
+template <typename T, int TPR, int NV, bool GRAD>
+__global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void k_loss(Rows q, LossArgs a, LossOut o) {
+    constexpr int WG = TPR < kThreads ? kThreads : TPR, N = kVec<T>;
+    __shared__ Sums red[2][16];
+    __shared__ double part[WG / TPR][3];
+    int half = 0;
+    const int t = threadIdx.x % TPR;
+    double acc[3] = {0.0, 0.0, 0.0};
+    for (int64_t r = (int64_t)blockIdx.x * (WG / TPR) + threadIdx.x / TPR; r < q.M; r += (int64_t)gridDim.x * (WG / TPR)) {
+        const T *z = static_cast<const T *>(q.z) + r * q.ld;
+        T *dz = static_cast<T *>(o.dz) + r * o.ld_d;
+        const Parts<T> parts(z, q.a);
+        const T *body = z + parts.head;
+        const float w = a.weight ? a.weight[r] : a.inv_m;
+        const bool same = GRAD && ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(dz)) & 15) == 0;
+        if (w == 0.f) {  // padding
+            if (GRAD) {
+                const float zero[N] = {};
+                for (int v = t; v < parts.full; v += TPR) store_vec<T>(dz, parts.head + v * N, zero, same);
+                const int i = parts.edge(t);
+                if (i >= 0) store(dz + i, 0.f);
+            }
+            if (t == 0 && o.logp) o.logp[r] = 0.f;
+            continue;
+        }
+        uint4 raw[NV];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int v = t + TPR * j;
+            raw[j] = v < parts.full ? *reinterpret_cast<const uint4 *>(body + (int64_t)v * N) : all_excluded<T>();
+        }
+        const int act = min(max(q.act[r], 0), q.a - 1);
+        const float zact = to_f32(z[act]), old = a.logp_old[r], adv = a.adv[r];
+        const float ref = a.logp_ref ? a.logp_ref[r] : 0.f;
+        const int ei = parts.edge(t);
+        float ex = ei < 0 ? -INFINITY : to_f32(z[ei]);
+        Sums sum{-INFINITY, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            float x[N];
+            unpack(raw[j], x);
+            add_values<N>(sum, x);
+        }
+        for (int v = t + TPR * NV; v < parts.full; v += TPR) {  // what the registers do not hold
+            float x[N];
+            unpack(*reinterpret_cast<const uint4 *>(body + (int64_t)v * N), x);
+            add_values<N>(sum, x);
+        }
+        if (parts.head + parts.tail > 0) {
+            const float x[1] = {ex};
+            add_values<1>(sum, x);
+        }
+        sum = row_join<TPR>(sum, red, half);
+        const float l2s = __builtin_amdgcn_logf(sum.s);
+        const float mean_y = sum.u / sum.s;
+        const float lsum = fmaf(l2s, kLn2, (float)(kLog2eRest * kLn2d * kLn2d) * mean_y);
+        const float logp = sum.s == 0.f ? 0.f : (zact - sum.m) - lsum;
+        const float H = sum.s == 0.f ? 0.f : lsum - kLn2 * mean_y;
+        float gl, ge;
+        loss_grad(a, w, old, ref, adv, logp, gl, ge);
+        if (t == 0) {
+            double term[3];
+            loss_row(a, r, w, (double)logp, (double)H, term);
+            for (int c = 0; c < 3; ++c) acc[c] += term[c];
+            if (o.logp) o.logp[r] = logp;
+        }
+        if (!GRAD) continue;
+        const RowCoef k = coef_of(sum.m, sum.s, l2s, H, gl, ge);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int v = t + TPR * j;
+            if (v < parts.full) grad_vec<T>(dz, parts.head + v * N, raw[j], k, same);
+        }
+        for (int v = t + TPR * NV; v < parts.full; v += TPR)
+            grad_vec<T>(dz, parts.head + v * N, *reinterpret_cast<const uint4 *>(body + (int64_t)v * N), k, same);
+        if (ei >= 0) store(dz + ei, k.zero != 0.f ? 0.f : grad_any(k, ex));
+        // the chosen action's column once more, by the thread that wrote it
+        const int av = (act - parts.head) / N;
+        const bool mine = act < parts.head || act >= parts.head + parts.full * N ? ei == act : av % TPR == t;
+        if (mine && k.zero == 0.f) store(dz + act, grad_any(k, zact) + k.g);
+    }
+    if (t == 0)
+        for (int c = 0; c < 3; ++c) part[threadIdx.x / TPR][c] = acc[c];
+    __syncthreads();
+    if (threadIdx.x < 3) {
+        double s = 0.0;
+        for (int i = 0; i < WG / TPR; ++i) s += part[i][threadIdx.x];
+        o.terms[(int64_t)blockIdx.x * 3 + threadIdx.x] = s;
+    }
+}
+
+// ---- preference loss ----
+// A row for the gradient pass of one segment: m, log2 s and the gradient of its log-probability.
+struct RowFin {
+    float m, l2s, g, pad;
+};
 
 struct PairArgs {
     const float *logp_ref, *weight;
     const int32_t *seq_ptr;
-    int n_rows, n_seg, n_pairs;
+    int n_rows, n_seg, chunks, n_pairs;
     float beta, smoothing;
 };
 
-// Pair p by workgroup p (stepping over pairs): both tracks' log ratios, the loss terms and, with
-// grad, every row's gradient.
-__global__ __launch_bounds__(kThreads) void k_pairs(PairArgs a, const Stat *__restrict__ stat, RowGrad *__restrict__ grad,
-                                                    double *__restrict__ terms, float *__restrict__ ratio) {
+// Pair p by workgroup p (stepping over pairs): both tracks' log ratios, the loss terms and every row's
+// gradient (fin for one segment, whose statistics are `chunks` parts a row; else grad).
+__global__ __launch_bounds__(kThreads) void k_pairs(PairArgs a, const Stat *__restrict__ stat, RowFin *__restrict__ fin,
+                                                    RowGrad *__restrict__ grad, double *__restrict__ terms,
+                                                    float *__restrict__ ratio) {
     __shared__ double part[kThreads];
     for (int64_t p = blockIdx.x; p < a.n_pairs; p += gridDim.x) {
         double R[2];
@@ -235,7 +648,16 @@ __global__ __launch_bounds__(kThreads) void k_pairs(PairArgs a, const Stat *__re
                 const float w = a.weight ? a.weight[r] : 1.f;
                 if (w == 0.f) continue;
                 double lp = a.logp_ref ? -(double)a.logp_ref[r] : 0.0;
-                for (int k = 0; k < a.n_seg; ++k) lp += stat_logp(stat[r * a.n_seg + k]);
+                if (a.n_seg == 1) {
+                    const Sums q = join_chunks(stat + r * a.chunks, a.chunks);
+                    lp += log_prob(q, stat[r * a.chunks].zact);
+                    if (fin) {
+                        fin[r].m = q.s == 0.f ? -INFINITY : q.m;
+                        fin[r].l2s = (float)(log((double)q.s) * 1.4426950408889634);
+                    }
+                } else {
+                    for (int k = 0; k < a.n_seg; ++k) lp += stat_logp(stat[r * a.n_seg + k]);
+                }
                 s += (double)w * lp;
             }
             part[threadIdx.x] = s;
@@ -261,23 +683,164 @@ __global__ __launch_bounds__(kThreads) void k_pairs(PairArgs a, const Stat *__re
                 ratio[2 * p + 1] = (float)R[1];
             }
         }
-        if (!grad) continue;
+        if (!fin && !grad) continue;
         const double g = (double)a.beta * ((double)a.smoothing - down) / (double)a.n_pairs;
         for (int side = 0; side < 2; ++side) {
             const int lo = clamp_row(a.seq_ptr[2 * p + side], a.n_rows), hi = clamp_row(a.seq_ptr[2 * p + side + 1], a.n_rows);
             for (int64_t r = (int64_t)lo + threadIdx.x; r < hi; r += kThreads) {
                 const float w = a.weight ? a.weight[r] : 1.f;
-                grad[r] = RowGrad{w == 0.f ? 0.f : (float)((double)w * (side ? -g : g)), 0.f};
+                const float gr = w == 0.f ? 0.f : (float)((double)w * (side ? -g : g));
+                if (fin) fin[r].g = gr;
+                else grad[r] = RowGrad{gr, 0.f};
             }
         }
     }
 }
 
-__global__ __launch_bounds__(kThreads) void k_pairs_sum(const double *__restrict__ terms, int n_pairs, float *__restrict__ loss) {
+__device__ __forceinline__ void pairs_sum(const double *__restrict__ terms, int n_pairs, float *__restrict__ loss) {
     double s[4];
     sum_terms<4>(terms, n_pairs, s);
     if (threadIdx.x == 0)
         for (int c = 0; c < 4; ++c) loss[c] = (float)(s[c] / (double)n_pairs);
+}
+
+__global__ __launch_bounds__(kThreads) void k_pairs_sum(const double *__restrict__ terms, int n_pairs, float *__restrict__ loss) {
+    pairs_sum(terms, n_pairs, loss);
+}
+
+// ---- the gradient of rows whose sums are known, an item (row, chunk) a workgroup ----
+enum Src : int { kFromFin = 0, kFromLse = 1, kFromLoss = 2 };
+
+struct GradSrc {
+    const RowFin *fin;                                     // kFromFin
+    const float *lse, *entropy, *g_logp, *g_entropy;       // kFromLse
+    const Stat *stat;                                      // kFromLoss: [row][stat_chunks]
+    int stat_chunks;
+    LossArgs loss;                                         // kFromLoss
+    float *logp;
+    // the launch's last workgroup sums the loss: over n_pairs pairs' terms (kFromFin) or over the rows (kFromLoss)
+    float *loss_out;
+    const double *terms;
+    int n_pairs;
+    void *dz;
+    int64_t ld_d;
+};
+
+// kFromLoss: row r's sums from its chunks, by one wave.
+__device__ __forceinline__ Sums join_wave(const Stat *__restrict__ st, int chunks, float &zact) {
+    const int l = threadIdx.x % 64;
+    Sums q{-INFINITY, 0.f, 0.f};
+    if (l < chunks) {
+        const Stat x = st[l];
+        q = Sums{x.m, x.s, x.u};
+    }
+    zact = st[0].zact;
+    q = lanes_join<64>(q);
+    if (!(q.m < INFINITY)) q.s = q.u = __builtin_nanf("");
+    return q;
+}
+
+// Few rows' loss terms by one workgroup: a thread a row where rows have few chunks, else a wave a row.
+__device__ void loss_of_rows(const GradSrc &a, int M) {
+    __shared__ double part[3][kThreads];
+    double acc[3] = {0.0, 0.0, 0.0};
+    const bool wave = a.stat_chunks > 16;
+    const int step = wave ? kThreads / 64 : kThreads;
+    for (int r = wave ? (int)threadIdx.x / 64 : (int)threadIdx.x; r < M; r += step) {
+        const float w = a.loss.weight ? a.loss.weight[r] : a.loss.inv_m;
+        if (w == 0.f) {
+            if (a.logp && (!wave || threadIdx.x % 64 == 0)) a.logp[r] = 0.f;
+            continue;
+        }
+        const Stat *st = a.stat + (int64_t)r * a.stat_chunks;
+        float zact = st[0].zact;
+        const Sums q = wave ? join_wave(st, a.stat_chunks, zact) : join_chunks(st, a.stat_chunks);
+        if (wave && threadIdx.x % 64) continue;
+        const double lp = log_prob(q, zact);
+        double term[3];
+        loss_row(a.loss, r, w, lp, entropy_of(q), term);
+        for (int c = 0; c < 3; ++c) acc[c] += term[c];
+        if (a.logp) a.logp[r] = (float)lp;
+    }
+    for (int c = 0; c < 3; ++c) part[c][threadIdx.x] = acc[c];
+    __syncthreads();
+    for (int h = kThreads / 2; h > 0; h >>= 1) {
+        if ((int)threadIdx.x < h)
+            for (int c = 0; c < 3; ++c) part[c][threadIdx.x] += part[c][threadIdx.x + h];
+        __syncthreads();
+    }
+    if (threadIdx.x == 0 && a.loss_out) {
+        const double s[3] = {part[0][0], part[1][0], part[2][0]};
+        write_loss(s, a.loss.w_kl, a.loss.w_entropy, a.loss_out);
+    }
+}
+
+template <typename T, int SRC>
+__global__ __launch_bounds__(kThreads) void k_grad(Rows q, int chunks, int per, GradSrc a) {
+    constexpr int N = kVec<T>, NV = 4;
+    const int64_t items = (int64_t)q.M * chunks;
+    if (SRC != kFromLse && blockIdx.x == gridDim.x - 1) {  // the workgroup behind the items' ones
+        if (SRC == kFromLoss) loss_of_rows(a, q.M);
+        else if (a.loss_out) pairs_sum(a.terms, a.n_pairs, a.loss_out);
+        return;
+    }
+    const int64_t step = SRC == kFromLse ? gridDim.x : gridDim.x - 1;
+    const int t = threadIdx.x;
+    for (int64_t it = blockIdx.x; it < items; it += step) {
+        const int r = chunks == 1 ? (int)it : (int)(it / chunks), c = (int)(it - (int64_t)r * chunks);
+        if (q.seq_ptr && (r < clamp_row(q.seq_ptr[0], q.M) || r >= clamp_row(q.seq_ptr[q.n_seq], q.M))) continue;
+        const T *z = static_cast<const T *>(q.z) + (int64_t)r * q.ld;
+        T *dz = static_cast<T *>(a.dz) + (int64_t)r * a.ld_d;
+        const Parts<T> parts(z, q.a);
+        const T *body = z + parts.head;
+        const bool same = ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(dz)) & 15) == 0;
+        const int act = min(max(q.act[r], 0), q.a - 1);
+        RowCoef k{};
+        float hot = 0.f;  // the gradient at the action
+        if (SRC == kFromFin) {
+            const RowFin f = a.fin[r];
+            k = coef_of(f.m, f.m == -INFINITY ? 0.f : 1.f, f.l2s, 0.f, f.g, 0.f);
+        } else if (SRC == kFromLse) {
+            const float m = a.lse[2 * (int64_t)r], ge = a.g_entropy ? a.g_entropy[r] : 0.f;
+            k = coef_of(m, m == -INFINITY ? 0.f : 1.f, a.lse[2 * (int64_t)r + 1] * kLog2e, ge != 0.f ? a.entropy[r] : 0.f, a.g_logp[r], ge);
+        } else {
+            const float w = a.loss.weight ? a.loss.weight[r] : a.loss.inv_m;
+            k.zero = 1.f;
+            if (w != 0.f) {
+                float zact;
+                const Sums s = join_wave(a.stat + (int64_t)r * a.stat_chunks, a.stat_chunks, zact);
+                const float H = (float)entropy_of(s), logp = (float)log_prob(s, zact);
+                float gl, ge;
+                loss_grad(a.loss, w, a.loss.logp_old[r], a.loss.logp_ref ? a.loss.logp_ref[r] : 0.f, a.loss.adv[r], logp, gl, ge);
+                k = coef_of(s.m, s.s, __builtin_amdgcn_logf(s.s), H, gl, ge);
+                hot = grad_any(k, zact) + k.g;
+            }
+        }
+        const int v1 = min((c + 1) * per, parts.full);
+        const int av = act >= parts.head && act < parts.head + parts.full * N ? (act - parts.head) / N : -1;
+        for (int v = c * per + t; v < v1; v += kThreads * NV) {
+            uint4 raw[NV];
+            if (k.zero == 0.f) {
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+                    if (v + kThreads * j < v1) raw[j] = *reinterpret_cast<const uint4 *>(body + (int64_t)(v + kThreads * j) * N);
+            }
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                const int vj = v + kThreads * j;
+                if (vj >= v1) break;
+                // kFromFin and kFromLse: the chosen action's logit lies in its own vector
+                float za = 0.f;
+                if (SRC != kFromLoss && vj == av && k.zero == 0.f) za = to_f32(z[act]);
+                grad_vec<T>(dz, parts.head + vj * N, raw[j], k, same);
+                if (vj == av && k.zero == 0.f) store(dz + act, SRC == kFromLoss ? hot : grad_any(k, za) + k.g);
+            }
+        }
+        if (c == 0) {
+            const int i = parts.edge(t);
+            if (i >= 0) store(dz + i, k.zero != 0.f ? 0.f : grad_any(k, to_f32(z[i])) + (i == act ? k.g : 0.f));
+        }
+    }
 }
 
 struct GradArgs {
@@ -362,15 +925,85 @@ int launch_grad(const harl_policy_head *h, const Rows &q, const GradArgs &a, hip
     return HARL_OK;
 }
 
-// The workspace: stats per (row, segment), gradients per row, loss terms per row or pair.
+// ---- launch shapes of one-segment heads ----
+int vec_of(const harl_policy_head *h) { return h->dtype == HARL_BF16 ? 8 : 4; }
+
+constexpr int kSplitItems = 1024;  // items that a launch of few rows is cut into
+constexpr int kMaxChunks = 64;     // a wave joins a row's chunks
+constexpr int kLossGrid = 8192;    // workgroups of k_loss: its terms
+
+// Chunks of a row: rows that leave the machine idle are cut until there are about kSplitItems items, none of
+// fewer than 512 vectors (two a thread).
+int chunks_for(const harl_policy_head *h, int32_t M) {
+    const int64_t vecs = h->a / vec_of(h);
+    return (int)std::max<int64_t>(1, std::min<int64_t>({ceil_div(kSplitItems, M), (int64_t)kMaxChunks, vecs / 512}));
+}
+
+template <typename T, int OUT>
+void launch_stats_as(const Rows &q, int chunks, const StatOut &o, hipStream_t stream) {
+    const int per = (int)ceil_div(std::max(q.a / kVec<T>, 1), chunks);
+    const int64_t items = (int64_t)q.M * chunks;
+    if (chunks == 1 && q.a / kVec<T> <= 512)  // a wave a row: no barrier, four rows a workgroup
+        hipLaunchKernelGGL((k_stats<T, 64, 4, OUT>), dim3(grid_for(ceil_div(items, 4))), dim3(kThreads), 0, stream, q, chunks, per, o);
+    else
+        hipLaunchKernelGGL((k_stats<T, 256, 4, OUT>), dim3(grid_for(items)), dim3(kThreads), 0, stream, q, chunks, per, o);
+}
+
+template <int OUT>
+int launch_wide_stats(const harl_policy_head *h, const Rows &q, int chunks, const StatOut &o, hipStream_t stream) {
+    if (h->dtype == HARL_BF16) launch_stats_as<uint16_t, OUT>(q, chunks, o, stream);
+    else launch_stats_as<float, OUT>(q, chunks, o, stream);
+    HARL_HIP_CHECK(hipGetLastError());
+    return HARL_OK;
+}
+
+template <int SRC>
+int launch_wide_grad(const harl_policy_head *h, const Rows &q, const GradSrc &a, hipStream_t stream) {
+    const int vecs = std::max(h->a / vec_of(h), 1);
+    const int chunks = (int)ceil_div(vecs, 1024), per = (int)ceil_div(vecs, chunks);
+    const unsigned grid = (a.dz ? grid_for((int64_t)q.M * chunks) : 0) + (SRC == kFromLse ? 0 : 1);
+    if (h->dtype == HARL_BF16)
+        hipLaunchKernelGGL((k_grad<uint16_t, SRC>), dim3(grid), dim3(kThreads), 0, stream, q, chunks, per, a);
+    else
+        hipLaunchKernelGGL((k_grad<float, SRC>), dim3(grid), dim3(kThreads), 0, stream, q, chunks, per, a);
+    HARL_HIP_CHECK(hipGetLastError());
+    return HARL_OK;
+}
+
+template <typename T, int TPR, int NV>
+unsigned launch_loss_as(const Rows &q, const LossArgs &a, const LossOut &o, hipStream_t stream) {
+    constexpr int WG = TPR < kThreads ? kThreads : TPR;
+    const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(q.M, WG / TPR), kLossGrid);
+    if (o.dz) hipLaunchKernelGGL((k_loss<T, TPR, NV, true>), dim3(grid), dim3(WG), 0, stream, q, a, o);
+    else hipLaunchKernelGGL((k_loss<T, TPR, NV, false>), dim3(grid), dim3(WG), 0, stream, q, a, o);
+    return grid;
+}
+
+// The shape whose registers hold a row; the widest rows go in part through memory twice.
+template <typename T>
+unsigned launch_loss(const Rows &q, const LossArgs &a, const LossOut &o, hipStream_t stream) {
+    const int v = q.a / kVec<T>;
+    if (v <= 64) return launch_loss_as<T, 64, 1>(q, a, o, stream);
+    if (v <= 128) return launch_loss_as<T, 64, 2>(q, a, o, stream);
+    if (v <= 256) return launch_loss_as<T, 64, 4>(q, a, o, stream);
+    if (v <= 512) return launch_loss_as<T, 64, 8>(q, a, o, stream);
+    if (v <= 1024) return launch_loss_as<T, 256, 4>(q, a, o, stream);
+    if (v <= 2048) return launch_loss_as<T, 256, 8>(q, a, o, stream);
+    if (v <= 4096) return launch_loss_as<T, 256, 16>(q, a, o, stream);
+    if (v <= 8192) return launch_loss_as<T, 512, 16>(q, a, o, stream);
+    return launch_loss_as<T, 1024, 16>(q, a, o, stream);
+}
+
+// The workspace: statistics per (row, segment) or (row, chunk), per-row gradients, loss terms.
 struct Ws {
     Stat *stat;
     RowGrad *grad;
+    RowFin *fin;
     double *terms;
     size_t bytes;
 };
 
-Ws ws_layout(const harl_policy_head *h, int64_t rows, int64_t n_terms, char *base) {
+Ws ws_layout(int64_t n_stat, int64_t n_grad, int64_t n_fin, int64_t n_terms, char *base) {
     Ws w{};
     int64_t off = 0;
     auto take = [&](int64_t bytes) {
@@ -378,29 +1011,50 @@ Ws ws_layout(const harl_policy_head *h, int64_t rows, int64_t n_terms, char *bas
         off += round_up(std::max<int64_t>(bytes, 1), 256);
         return p;
     };
-    w.stat = reinterpret_cast<Stat *>(take(rows * h->n_seg * (int64_t)sizeof(Stat)));
-    w.grad = reinterpret_cast<RowGrad *>(take(rows * (int64_t)sizeof(RowGrad)));
+    w.stat = reinterpret_cast<Stat *>(take(n_stat * (int64_t)sizeof(Stat)));
+    w.grad = reinterpret_cast<RowGrad *>(take(n_grad * (int64_t)sizeof(RowGrad)));
+    w.fin = reinterpret_cast<RowFin *>(take(n_fin * (int64_t)sizeof(RowFin)));
     w.terms = reinterpret_cast<double *>(take(n_terms * 8));
     w.bytes = (size_t)off;
     return w;
 }
 
-}  // namespace
-
-size_t objective_logp_ws_bytes(const harl_policy_head *head, int32_t M) { return ws_layout(head, M, 0, nullptr).bytes; }
-
-size_t objective_loss_ws_bytes(const harl_policy_head *head, int32_t M) {
-    return ws_layout(head, M, 3 * (int64_t)M, nullptr).bytes;
+// Few rows in chunks: at most rows + kSplitItems items.
+Ws logp_ws(const harl_policy_head *h, int64_t M, char *base) {
+    return h->n_seg == 1 ? ws_layout(std::min<int64_t>(M, kSplitItems) + kSplitItems, 0, 0, 0, base)
+                         : ws_layout(M * h->n_seg, 0, 0, 0, base);
+}
+Ws loss_ws(const harl_policy_head *h, int64_t M, char *base) {
+    return h->n_seg == 1 ? ws_layout(std::min<int64_t>(M, kSplitItems) + kSplitItems, 0, 0, 3 * std::min<int64_t>(M, kLossGrid), base)
+                         : ws_layout(M * h->n_seg, M, 0, 3 * M, base);
+}
+Ws preference_ws(const harl_policy_head *h, int64_t rows, int64_t pairs, char *base) {
+    return h->n_seg == 1 ? ws_layout(rows + kSplitItems, 0, rows, 4 * pairs, base) : ws_layout(rows * h->n_seg, rows, 0, 4 * pairs, base);
 }
 
+}  // namespace
+
+size_t objective_logp_ws_bytes(const harl_policy_head *head, int32_t M) { return logp_ws(head, M, nullptr).bytes; }
+
+size_t objective_loss_ws_bytes(const harl_policy_head *head, int32_t M) { return loss_ws(head, M, nullptr).bytes; }
+
 size_t objective_preference_ws_bytes(const harl_policy_head *head, int32_t n_rows, int32_t n_pairs) {
-    return ws_layout(head, n_rows, 4 * (int64_t)n_pairs, nullptr).bytes;
+    return preference_ws(head, n_rows, n_pairs, nullptr).bytes;
 }
 
 int policy_logp_launch(const harl_policy_head *head, const void *logits, int64_t ld, int32_t M, const int32_t *actions,
                        float *logp, float *entropy, float *lse, void *ws, hipStream_t stream) {
-    const Ws w = ws_layout(head, M, 0, static_cast<char *>(ws));
+    const Ws w = logp_ws(head, M, static_cast<char *>(ws));
     const Rows q = rows_of(head, logits, ld, M, actions);
+    if (head->n_seg == 1) {
+        const int chunks = chunks_for(head, M);
+        const StatOut o{w.stat, logp, entropy, lse};
+        if (chunks == 1) return launch_wide_stats<kLogp>(head, q, 1, o, stream);
+        if (const int rc = launch_wide_stats<kPartial>(head, q, chunks, o, stream)) return rc;
+        hipLaunchKernelGGL(k_logp_join, dim3(grid_for(ceil_div(M, 64))), dim3(64), 0, stream, w.stat, M, chunks, o);
+        HARL_HIP_CHECK(hipGetLastError());
+        return HARL_OK;
+    }
     if (const int rc = launch_stats(head, q, w.stat, stream)) return rc;
     hipLaunchKernelGGL(k_logp_rows, dim3(grid_for(ceil_div(M, kThreads))), dim3(kThreads), 0, stream, w.stat, M,
                        head->n_seg, logp, entropy, lse);
@@ -411,6 +1065,17 @@ int policy_logp_launch(const harl_policy_head *head, const void *logits, int64_t
 int policy_logp_grad_launch(const harl_policy_head *head, const void *logits, int64_t ld, int32_t M,
                             const int32_t *actions, const float *lse, const float *entropy, const float *g_logp,
                             const float *g_entropy, void *dlogits, int64_t ld_d, hipStream_t stream) {
+    const Rows q = rows_of(head, logits, ld, M, actions);
+    if (head->n_seg == 1) {
+        GradSrc a{};
+        a.lse = lse;
+        a.entropy = entropy;
+        a.g_logp = g_logp;
+        a.g_entropy = g_entropy;
+        a.dz = dlogits;
+        a.ld_d = ld_d;
+        return launch_wide_grad<kFromLse>(head, q, a, stream);
+    }
     GradArgs a{};
     a.lse = lse;
     a.entropy = entropy;
@@ -418,27 +1083,47 @@ int policy_logp_grad_launch(const harl_policy_head *head, const void *logits, in
     a.g_entropy = g_entropy;
     a.dz = dlogits;
     a.ld_d = ld_d;
-    return launch_grad(head, rows_of(head, logits, ld, M, actions), a, stream);
+    return launch_grad(head, q, a, stream);
 }
 
 int policy_loss_launch(const harl_policy_head *head, const harl_policy_loss_config *cfg, const void *logits, int64_t ld,
                        int32_t M, const int32_t *actions, const float *logp_old, const float *logp_ref,
                        const float *adv, const float *weight, void *dlogits, int64_t ld_d, float *logp, float *loss,
                        void *ws, hipStream_t stream) {
-    const Ws w = ws_layout(head, M, 3 * (int64_t)M, static_cast<char *>(ws));
+    const Ws w = loss_ws(head, M, static_cast<char *>(ws));
     Rows q = rows_of(head, logits, ld, M, actions);
     q.weight = weight;
-    if (const int rc = launch_stats(head, q, w.stat, stream)) return rc;
-    LossArgs a{logp_old, logp_ref, adv, weight, cfg->clip_low, cfg->clip_high, cfg->w_kl, cfg->w_entropy, 1.f / (float)M};
-    hipLaunchKernelGGL(k_loss_rows, dim3(grid_for(ceil_div(M, kThreads))), dim3(kThreads), 0, stream, a, w.stat, M,
-                       head->n_seg, w.grad, w.terms, logp);
-    HARL_HIP_CHECK(hipGetLastError());
-    if (loss) {
-        hipLaunchKernelGGL(k_loss_sum, dim3(1), dim3(kThreads), 0, stream, w.terms, (int64_t)M, cfg->w_kl,
-                           cfg->w_entropy, loss);
+    const LossArgs a{logp_old, logp_ref, adv, weight, cfg->clip_low, cfg->clip_high, cfg->w_kl, cfg->w_entropy, 1.f / (float)M};
+    int64_t n_terms = M;
+    if (head->n_seg == 1) {
+        const int chunks = chunks_for(head, M);
+        if (chunks > 1) {
+            const StatOut o{w.stat, nullptr, nullptr, nullptr};
+            if (const int rc = launch_wide_stats<kPartial>(head, q, chunks, o, stream)) return rc;
+            GradSrc g{};
+            g.stat = w.stat;
+            g.stat_chunks = chunks;
+            g.loss = a;
+            g.logp = logp;
+            g.loss_out = loss;
+            g.dz = dlogits;
+            g.ld_d = ld_d;
+            return launch_wide_grad<kFromLoss>(head, q, g, stream);
+        }
+        const LossOut o{dlogits, ld_d, logp, w.terms};
+        n_terms = head->dtype == HARL_BF16 ? launch_loss<uint16_t>(q, a, o, stream) : launch_loss<float>(q, a, o, stream);
+        HARL_HIP_CHECK(hipGetLastError());
+    } else {
+        if (const int rc = launch_stats(head, q, w.stat, stream)) return rc;
+        hipLaunchKernelGGL(k_loss_rows, dim3(grid_for(ceil_div(M, kThreads))), dim3(kThreads), 0, stream, a, w.stat, M,
+                           head->n_seg, w.grad, w.terms, logp);
         HARL_HIP_CHECK(hipGetLastError());
     }
-    if (!dlogits) return HARL_OK;
+    if (loss) {
+        hipLaunchKernelGGL(k_loss_sum, dim3(1), dim3(kThreads), 0, stream, w.terms, n_terms, cfg->w_kl, cfg->w_entropy, loss);
+        HARL_HIP_CHECK(hipGetLastError());
+    }
+    if (!dlogits || head->n_seg == 1) return HARL_OK;
     GradArgs g{};
     g.stat = w.stat;
     g.grad = w.grad;
@@ -451,18 +1136,32 @@ int preference_loss_launch(const harl_policy_head *head, const harl_preference_c
                            int64_t ld, int32_t n_rows, const int32_t *actions, const float *logp_ref,
                            const float *weight, const int32_t *seq_ptr, int32_t n_pairs, void *dlogits, int64_t ld_d,
                            float *ratio, float *loss, void *ws, hipStream_t stream) {
-    const Ws w = ws_layout(head, n_rows, 4 * (int64_t)n_pairs, static_cast<char *>(ws));
+    const Ws w = preference_ws(head, n_rows, n_pairs, static_cast<char *>(ws));
     Rows q = rows_of(head, logits, ld, n_rows, actions);
     q.weight = weight;
     q.seq_ptr = seq_ptr;
     q.n_seq = 2 * n_pairs;
-    const bool grad = dlogits && n_rows > 0;
-    if (n_rows > 0)
-        if (const int rc = launch_stats(head, q, w.stat, stream)) return rc;
-    PairArgs a{logp_ref, weight, seq_ptr, n_rows, head->n_seg, n_pairs, cfg->beta, cfg->smoothing};
-    hipLaunchKernelGGL(k_pairs, dim3(grid_for(n_pairs)), dim3(kThreads), 0, stream, a, w.stat, grad ? w.grad : nullptr,
-                       w.terms, ratio);
+    const bool grad = dlogits && n_rows > 0, wide = head->n_seg == 1;
+    const int chunks = wide && n_rows > 0 ? chunks_for(head, n_rows) : 1;
+    if (n_rows > 0) {
+        const StatOut o{w.stat, nullptr, nullptr, nullptr};
+        if (const int rc = wide ? launch_wide_stats<kPartial>(head, q, chunks, o, stream) : launch_stats(head, q, w.stat, stream))
+            return rc;
+    }
+    const PairArgs a{logp_ref, weight, seq_ptr, n_rows, head->n_seg, chunks, n_pairs, cfg->beta, cfg->smoothing};
+    hipLaunchKernelGGL(k_pairs, dim3(grid_for(n_pairs)), dim3(kThreads), 0, stream, a, w.stat, grad && wide ? w.fin : nullptr,
+                       grad && !wide ? w.grad : nullptr, w.terms, ratio);
     HARL_HIP_CHECK(hipGetLastError());
+    if (grad && wide) {
+        GradSrc g{};
+        g.fin = w.fin;
+        g.loss_out = loss;
+        g.terms = w.terms;
+        g.n_pairs = n_pairs;
+        g.dz = dlogits;
+        g.ld_d = ld_d;
+        return launch_wide_grad<kFromFin>(head, q, g, stream);
+    }
     if (loss) {
         hipLaunchKernelGGL(k_pairs_sum, dim3(1), dim3(kThreads), 0, stream, w.terms, n_pairs, loss);
         HARL_HIP_CHECK(hipGetLastError());
