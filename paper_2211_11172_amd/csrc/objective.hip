@@ -517,16 +517,70 @@ struct LossOut {
     double *terms;  // [workgroup][3]: the sums of its rows' terms, in row order
 };
 
-// loss_row in fp32: every wave of a row evaluates this.
-__device__ __forceinline__ void loss_grad(const LossArgs &a, float w, float old, float ref, float adv, float logp, float &gl, float &ge) {
+// loss_row in fp32, evaluated by every wave of a row: in 64 bits it takes 100 registers beside the row's.
+// e^x - x - 1 near 0 comes from its series, where the difference would cancel.
+__device__ __forceinline__ void loss_grad(const LossArgs &a, float w, float old, float ref, float adv, float logp, float &gl,
+                                          float &ge, float &surrogate, float &kl) {
     const float ratio = exp2_hw((logp - old) * kLog2e);
     const float lo = 1.f - a.clip_low, hi = 1.f + a.clip_high;
     const float s1 = ratio * adv, s2 = (ratio < lo ? lo : ratio > hi ? hi : ratio) * adv;
     const bool inside = ratio >= lo && ratio <= hi;
     const float ds = s2 < s1 && !inside ? 0.f : -s1;
-    const float dk = a.w_kl != 0.f ? a.w_kl * (1.f - exp2_hw((ref - logp) * kLog2e)) : 0.f;
+    float dk = 0.f;
+    kl = 0.f;
+    if (a.logp_ref) {
+        const float x = ref - logp, e = exp2_hw(x * kLog2e);
+        const float series = x * x * fmaf(x, fmaf(x, fmaf(x, fmaf(x, fmaf(x, 1.f / 5040.f, 1.f / 720.f), 1.f / 120.f), 1.f / 24.f), 1.f / 6.f), 0.5f);
+        kl = fabsf(x) < 0.25f ? series : x < INFINITY ? (e - 1.f) - x : x;
+        if (a.w_kl != 0.f) dk = a.w_kl * (1.f - e);
+    }
+    surrogate = s2 < s1 ? s2 : s1;
     gl = w * (ds + dk);
     ge = -w * a.w_entropy;
+}
+
+// A row's vectors as TPR-wide slices through buffer descriptors: thread t's vector of slice j lies at byte
+// 16 t of the slice, and the descriptor ends with the row (loads beyond give 0, stores go nowhere), so that
+// loads and stores need neither masks nor an address of their own a vector.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t slice(const void *base, int bytes, int from) {
+    char *p = static_cast<char *>(const_cast<void *>(base)) + from;
+    return __builtin_amdgcn_make_buffer_rsrc(p, 0, max(bytes - from, 0), 0x00027000);
+}
+__device__ __forceinline__ uint4 load_vec(__amdgpu_buffer_rsrc_t b, int byte) {
+    const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(b, byte, 0, 0);
+    return make_uint4(v.x, v.y, v.z, v.w);
+}
+__device__ __forceinline__ void put_vec(__amdgpu_buffer_rsrc_t b, int byte, const uint4 &v) {
+    __builtin_amdgcn_raw_buffer_store_b128(u32x4{v.x, v.y, v.z, v.w}, b, byte, 0, 0);
+}
+
+// The whole row dz = 0, or (other alignment than the logits') an element at a time from memory.
+template <typename T, int TPR>
+__device__ __forceinline__ void zero_row(T *dz, int a, int t) {
+    const Parts<T> parts(dz, a);
+    for (int v = t; v < parts.full; v += TPR) reinterpret_cast<uint4 *>(dz + parts.head)[v] = make_uint4(0, 0, 0, 0);
+    const int i = parts.edge(t);
+    if (i >= 0) store(dz + i, 0.f);
+}
+template <typename T, int TPR>
+__device__ __forceinline__ void grad_elements(const T *z, T *dz, int a, int act, const RowCoef &k, int t) {
+    for (int i = t; i < a; i += TPR) store(dz + i, grad_any(k, to_f32(z[i])) + (i == act ? k.g : 0.f));
+}
+
+template <typename T, int TPR, int NV, bool ENT>
+__device__ __forceinline__ void grad_slices(const T *dz_body, int full, const uint4 (&raw)[NV], const RowCoef &k, int t) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        if (TPR * j >= full) continue;  // uniform
+        float x[kVec<T>];
+        unpack(raw[j], x);
+#pragma unroll
+        for (int i = 0; i < kVec<T>; ++i) x[i] = grad_of<ENT>(k, x[i]);
+        put_vec(slice(dz_body, full * 16, TPR * 16 * j), t * 16, pack(x));
+        __builtin_amdgcn_sched_barrier(0);
+    }
 }
 
 template <typename T, int TPR, int NV, bool GRAD>
@@ -537,44 +591,40 @@ __global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void k_loss(Rows q
     int half = 0;
     const int t = threadIdx.x % TPR;
     double acc[3] = {0.0, 0.0, 0.0};
-    for (int64_t r = (int64_t)blockIdx.x * (WG / TPR) + threadIdx.x / TPR; r < q.M; r += (int64_t)gridDim.x * (WG / TPR)) {
+    for (int64_t r0 = (int64_t)blockIdx.x * (WG / TPR) + threadIdx.x / TPR; r0 < q.M; r0 += (int64_t)gridDim.x * (WG / TPR)) {
+        const int64_t r = __builtin_amdgcn_readfirstlane((int)r0);  // a wave lies in one row
         const T *z = static_cast<const T *>(q.z) + r * q.ld;
         T *dz = static_cast<T *>(o.dz) + r * o.ld_d;
-        const Parts<T> parts(z, q.a);
-        const T *body = z + parts.head;
         const float w = a.weight ? a.weight[r] : a.inv_m;
-        const bool same = GRAD && ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(dz)) & 15) == 0;
         if (w == 0.f) {  // padding
-            if (GRAD) {
-                const float zero[N] = {};
-                for (int v = t; v < parts.full; v += TPR) store_vec<T>(dz, parts.head + v * N, zero, same);
-                const int i = parts.edge(t);
-                if (i >= 0) store(dz + i, 0.f);
-            }
+            if (GRAD) zero_row<T, TPR>(dz, q.a, t);
             if (t == 0 && o.logp) o.logp[r] = 0.f;
             continue;
         }
+        const Parts<T> parts(z, q.a);
+        const int full = parts.full;
+        const T *body = z + parts.head;
         uint4 raw[NV];
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const int v = t + TPR * j;
-            raw[j] = v < parts.full ? *reinterpret_cast<const uint4 *>(body + (int64_t)v * N) : all_excluded<T>();
-        }
+        for (int j = 0; j < NV; ++j) raw[j] = load_vec(slice(body, full * 16, TPR * 16 * j), t * 16);
         const int act = min(max(q.act[r], 0), q.a - 1);
         const float zact = to_f32(z[act]), old = a.logp_old[r], adv = a.adv[r];
         const float ref = a.logp_ref ? a.logp_ref[r] : 0.f;
         const int ei = parts.edge(t);
-        float ex = ei < 0 ? -INFINITY : to_f32(z[ei]);
+        const float ex = ei < 0 ? -INFINITY : to_f32(z[ei]);
         Sums sum{-INFINITY, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
+            if (TPR * j >= full) continue;  // uniform
+            if (TPR * (j + 1) > full && t + TPR * j >= full) raw[j] = all_excluded<T>();
             float x[N];
             unpack(raw[j], x);
             add_values<N>(sum, x);
+            __builtin_amdgcn_sched_barrier(0);
         }
-        for (int v = t + TPR * NV; v < parts.full; v += TPR) {  // what the registers do not hold
+        for (int v = t + TPR * NV; v < full; v += TPR) {  // what the registers do not hold
             float x[N];
-            unpack(*reinterpret_cast<const uint4 *>(body + (int64_t)v * N), x);
+            unpack(reinterpret_cast<const uint4 *>(body)[v], x);
             add_values<N>(sum, x);
         }
         if (parts.head + parts.tail > 0) {
@@ -587,28 +637,31 @@ __global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void k_loss(Rows q
         const float lsum = fmaf(l2s, kLn2, (float)(kLog2eRest * kLn2d * kLn2d) * mean_y);
         const float logp = sum.s == 0.f ? 0.f : (zact - sum.m) - lsum;
         const float H = sum.s == 0.f ? 0.f : lsum - kLn2 * mean_y;
-        float gl, ge;
-        loss_grad(a, w, old, ref, adv, logp, gl, ge);
-        if (t == 0) {
-            double term[3];
-            loss_row(a, r, w, (double)logp, (double)H, term);
-            for (int c = 0; c < 3; ++c) acc[c] += term[c];
-            if (o.logp) o.logp[r] = logp;
-        }
+        float gl, ge, surrogate, kl;
+        loss_grad(a, w, old, ref, adv, logp, gl, ge, surrogate, kl);
+        acc[0] -= (double)w * (double)surrogate;
+        acc[1] += (double)w * (double)kl;
+        acc[2] += (double)w * (double)H;
+        if (t == 0 && o.logp) o.logp[r] = logp;
         if (!GRAD) continue;
         const RowCoef k = coef_of(sum.m, sum.s, l2s, H, gl, ge);
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const int v = t + TPR * j;
-            if (v < parts.full) grad_vec<T>(dz, parts.head + v * N, raw[j], k, same);
+        if (k.zero != 0.f) {
+            zero_row<T, TPR>(dz, q.a, t);
+            continue;
         }
-        for (int v = t + TPR * NV; v < parts.full; v += TPR)
-            grad_vec<T>(dz, parts.head + v * N, *reinterpret_cast<const uint4 *>(body + (int64_t)v * N), k, same);
-        if (ei >= 0) store(dz + ei, k.zero != 0.f ? 0.f : grad_any(k, ex));
+        if ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(dz)) & 15) {
+            grad_elements<T, TPR>(z, dz, q.a, act, k, t);
+            continue;
+        }
+        if (k.e != 0.f) grad_slices<T, TPR, NV, true>(dz + parts.head, full, raw, k, t);
+        else grad_slices<T, TPR, NV, false>(dz + parts.head, full, raw, k, t);
+        for (int v = t + TPR * NV; v < full; v += TPR)
+            grad_vec<T>(dz, parts.head + v * N, reinterpret_cast<const uint4 *>(body)[v], k, true);
+        if (ei >= 0) store(dz + ei, grad_any(k, ex));
         // the chosen action's column once more, by the thread that wrote it
         const int av = (act - parts.head) / N;
-        const bool mine = act < parts.head || act >= parts.head + parts.full * N ? ei == act : av % TPR == t;
-        if (mine && k.zero == 0.f) store(dz + act, grad_any(k, zact) + k.g);
+        const bool mine = act < parts.head || act >= parts.head + full * N ? ei == act : av % TPR == t;
+        if (mine) store(dz + act, grad_any(k, zact) + k.g);
     }
     if (t == 0)
         for (int c = 0; c < 3; ++c) part[threadIdx.x / TPR][c] = acc[c];
@@ -810,8 +863,9 @@ __global__ __launch_bounds__(kThreads) void k_grad(Rows q, int chunks, int per, 
                 float zact;
                 const Sums s = join_wave(a.stat + (int64_t)r * a.stat_chunks, a.stat_chunks, zact);
                 const float H = (float)entropy_of(s), logp = (float)log_prob(s, zact);
-                float gl, ge;
-                loss_grad(a.loss, w, a.loss.logp_old[r], a.loss.logp_ref ? a.loss.logp_ref[r] : 0.f, a.loss.adv[r], logp, gl, ge);
+                float gl, ge, surrogate, kl;
+                loss_grad(a.loss, w, a.loss.logp_old[r], a.loss.logp_ref ? a.loss.logp_ref[r] : 0.f, a.loss.adv[r], logp, gl, ge,
+                          surrogate, kl);
                 k = coef_of(s.m, s.s, __builtin_amdgcn_logf(s.s), H, gl, ge);
                 hot = grad_any(k, zact) + k.g;
             }
