@@ -32,12 +32,9 @@ struct Rows {
     int32_t off[HARL_SELECT_MAX_SEGMENTS + 1];
 };
 
-// A (row, segment)'s sums, and one row's gradients of log-probability and entropy.
+// A chunk of a row's sums, and the row's logit at its action.
 struct Stat {
     float m, s, u, zact;
-};
-struct RowGrad {
-    float g_logp, g_ent;
 };
 
 __device__ __forceinline__ float to_f32(float x) { return x; }
@@ -55,136 +52,25 @@ __device__ __forceinline__ bool row_counts(const Rows &q, int r) {
     return !q.weight || q.weight[r] != 0.f;
 }
 
-// Largest value (NaN if any is) and sum over a workgroup of kThreads; the result in every thread.
-__device__ __forceinline__ float block_max(float x, float *lds) {
-    lds[threadIdx.x] = x;
-    __syncthreads();
-    for (int h = kThreads / 2; h > 0; h >>= 1) {
-        if ((int)threadIdx.x < h) {
-            const float a = lds[threadIdx.x], b = lds[threadIdx.x + h];
-            lds[threadIdx.x] = b > a || b != b ? b : a;
-        }
-        __syncthreads();
-    }
-    const float r = lds[0];
-    __syncthreads();
-    return r;
-}
-__device__ __forceinline__ float block_sum(float x, float *lds) {
-    lds[threadIdx.x] = x;
-    __syncthreads();
-    for (int h = kThreads / 2; h > 0; h >>= 1) {
-        if ((int)threadIdx.x < h) lds[threadIdx.x] += lds[threadIdx.x + h];
-        __syncthreads();
-    }
-    const float r = lds[0];
-    __syncthreads();
-    return r;
-}
-
-template <typename T>
-__global__ __launch_bounds__(kThreads) void k_row_stats(Rows q, Stat *__restrict__ stat) {
-    __shared__ float lds[kThreads];
-    for (int64_t r = blockIdx.x; r < q.M; r += gridDim.x) {
-        if (!row_counts(q, (int)r)) continue;
-        const T *z = static_cast<const T *>(q.z) + r * q.ld;
-        for (int g = 0; g < q.n_seg; ++g) {
-            const int lo = q.off[g], hi = q.off[g + 1];
-            float m = -INFINITY;
-            for (int i = lo + (int)threadIdx.x; i < hi; i += kThreads) {
-                const float x = to_f32(z[i]);
-                m = x > m || x != x ? x : m;
-            }
-            m = block_max(m, lds);
-            float s = 0.f, u = 0.f;
-            if (m > -INFINITY || m != m)
-                for (int i = lo + (int)threadIdx.x; i < hi; i += kThreads) {
-                    const float d = to_f32(z[i]) - m;
-                    const float e = expf(d);
-                    s += e;
-                    u += e * fmaxf(d, -1000.f);  // an excluded action: 0, not 0 times -inf
-                }
-            s = block_sum(s, lds);
-            u = block_sum(u, lds);
-            if (threadIdx.x == 0) {
-                const int act = min(max(q.act[r * q.n_seg + g], lo), hi - 1);
-                stat[r * q.n_seg + g] = Stat{m, s, u, to_f32(z[act])};
-            }
-        }
-    }
-}
-
-// A segment's log-probability and entropy; an empty segment (s = 0) adds nothing.
-__device__ __forceinline__ double stat_logp(const Stat &t) {
-    return t.s == 0.f ? 0.0 : ((double)t.zact - (double)t.m) - log((double)t.s);
-}
-__device__ __forceinline__ double stat_entropy(const Stat &t) {
-    return t.s == 0.f ? 0.0 : log((double)t.s) - (double)t.u / (double)t.s;
-}
-
-__global__ __launch_bounds__(kThreads) void k_logp_rows(const Stat *__restrict__ stat, int M, int n_seg,
-                                                        float *__restrict__ logp, float *__restrict__ entropy,
-                                                        float *__restrict__ lse) {
-    for (int64_t r = (int64_t)blockIdx.x * kThreads + threadIdx.x; r < M; r += (int64_t)gridDim.x * kThreads) {
-        double lp = 0.0;
-        for (int g = 0; g < n_seg; ++g) {
-            const Stat t = stat[r * n_seg + g];
-            lp += stat_logp(t);
-            if (entropy) entropy[r * n_seg + g] = (float)stat_entropy(t);
-            if (lse) {
-                lse[(r * n_seg + g) * 2] = t.m;
-                lse[(r * n_seg + g) * 2 + 1] = t.s == 0.f ? 0.f : (float)log((double)t.s);
-            }
-        }
-        logp[r] = (float)lp;
-    }
-}
-
 struct LossArgs {
     const float *logp_old, *logp_ref, *adv, *weight;
     float clip_low, clip_high, w_kl, w_entropy;
     float inv_m;
 };
 
-// One row's terms of the clipped loss, weighted, and its gradients.
-__device__ __forceinline__ RowGrad loss_row(const LossArgs &a, int64_t r, float w, double logp, double H, double (&term)[3]) {
+// One row's terms of the clipped loss, weighted.
+__device__ __forceinline__ void loss_row(const LossArgs &a, int64_t r, float w, double logp, double H, double (&term)[3]) {
     const double ratio = exp(logp - (double)a.logp_old[r]);
     const double adv = a.adv[r], lo = 1.0 - (double)a.clip_low, hi = 1.0 + (double)a.clip_high;
     const double s1 = ratio * adv, s2 = (ratio < lo ? lo : ratio > hi ? hi : ratio) * adv;
-    const bool inside = ratio >= lo && ratio <= hi;
-    double kl = 0.0, dkl = 0.0;
+    double kl = 0.0;
     if (a.logp_ref) {
         const double x = (double)a.logp_ref[r] - logp;
-        dkl = -expm1(x);
-        kl = x < INFINITY ? -dkl - x : x;  // x = inf (an excluded action): inf, not inf - inf
+        kl = x < INFINITY ? expm1(x) - x : x;  // x = inf (an excluded action): inf, not inf - inf
     }
     term[0] = (double)w * -(s2 < s1 ? s2 : s1);
     term[1] = (double)w * kl;
     term[2] = (double)w * H;
-    const double d_surrogate = s2 < s1 && !inside ? 0.0 : -adv * ratio;
-    const double d_kl = a.w_kl != 0.f ? (double)a.w_kl * dkl : 0.0;
-    return RowGrad{(float)((double)w * (d_surrogate + d_kl)), -w * a.w_entropy};
-}
-
-__global__ __launch_bounds__(kThreads) void k_loss_rows(LossArgs a, const Stat *__restrict__ stat, int M, int n_seg,
-                                                        RowGrad *__restrict__ grad, double *__restrict__ terms,
-                                                        float *__restrict__ logp_out) {
-    for (int64_t r = (int64_t)blockIdx.x * kThreads + threadIdx.x; r < M; r += (int64_t)gridDim.x * kThreads) {
-        const float w = a.weight ? a.weight[r] : a.inv_m;
-        double term[3] = {0.0, 0.0, 0.0}, lp = 0.0, H = 0.0;
-        RowGrad g{0.f, 0.f};
-        if (w != 0.f) {
-            for (int k = 0; k < n_seg; ++k) {
-                const Stat t = stat[r * n_seg + k];
-                lp += stat_logp(t);
-                H += stat_entropy(t);
-            }
-            g = loss_row(a, r, w, lp, H, term);
-        }
-        grad[r] = g;
-        for (int c = 0; c < 3; ++c) terms[r * 3 + c] = term[c];
-        if (logp_out) logp_out[r] = (float)lp;
-    }
 }
 
 // Sums of N terms per row over n rows by one workgroup: thread-strided in row order, then a tree.
@@ -682,15 +568,16 @@ struct RowFin {
 struct PairArgs {
     const float *logp_ref, *weight;
     const int32_t *seq_ptr;
-    int n_rows, n_seg, chunks, n_pairs;
+    int n_rows, chunks, n_pairs;
     float beta, smoothing;
 };
 
 // Pair p by workgroup p (stepping over pairs): both tracks' log ratios, the loss terms and every row's
-// gradient (fin for one segment, whose statistics are `chunks` parts a row; else grad).
-__global__ __launch_bounds__(kThreads) void k_pairs(PairArgs a, const Stat *__restrict__ stat, RowFin *__restrict__ fin,
-                                                    RowGrad *__restrict__ grad, double *__restrict__ terms,
-                                                    float *__restrict__ ratio) {
+// gradient.  Rows come as `chunks` parts of statistics (one segment; their results go to fin) or as
+// weighted log ratios `diff` (several; their gradients go to g_row).
+__global__ __launch_bounds__(kThreads) void k_pairs(PairArgs a, const Stat *__restrict__ stat, const double *__restrict__ diff,
+                                                    RowFin *__restrict__ fin, float *__restrict__ g_row,
+                                                    double *__restrict__ terms, float *__restrict__ ratio) {
     __shared__ double part[kThreads];
     for (int64_t p = blockIdx.x; p < a.n_pairs; p += gridDim.x) {
         double R[2];
@@ -700,16 +587,15 @@ __global__ __launch_bounds__(kThreads) void k_pairs(PairArgs a, const Stat *__re
             for (int64_t r = (int64_t)lo + threadIdx.x; r < hi; r += kThreads) {
                 const float w = a.weight ? a.weight[r] : 1.f;
                 if (w == 0.f) continue;
-                double lp = a.logp_ref ? -(double)a.logp_ref[r] : 0.0;
-                if (a.n_seg == 1) {
-                    const Sums q = join_chunks(stat + r * a.chunks, a.chunks);
-                    lp += log_prob(q, stat[r * a.chunks].zact);
-                    if (fin) {
-                        fin[r].m = q.s == 0.f ? -INFINITY : q.m;
-                        fin[r].l2s = (float)(log((double)q.s) * 1.4426950408889634);
-                    }
-                } else {
-                    for (int k = 0; k < a.n_seg; ++k) lp += stat_logp(stat[r * a.n_seg + k]);
+                if (diff) {
+                    s += diff[r];
+                    continue;
+                }
+                const Sums q = join_chunks(stat + r * a.chunks, a.chunks);
+                const double lp = log_prob(q, stat[r * a.chunks].zact) - (a.logp_ref ? (double)a.logp_ref[r] : 0.0);
+                if (fin) {
+                    fin[r].m = q.s == 0.f ? -INFINITY : q.m;
+                    fin[r].l2s = (float)(log((double)q.s) * 1.4426950408889634);
                 }
                 s += (double)w * lp;
             }
@@ -736,7 +622,7 @@ __global__ __launch_bounds__(kThreads) void k_pairs(PairArgs a, const Stat *__re
                 ratio[2 * p + 1] = (float)R[1];
             }
         }
-        if (!fin && !grad) continue;
+        if (!fin && !g_row) continue;
         const double g = (double)a.beta * ((double)a.smoothing - down) / (double)a.n_pairs;
         for (int side = 0; side < 2; ++side) {
             const int lo = clamp_row(a.seq_ptr[2 * p + side], a.n_rows), hi = clamp_row(a.seq_ptr[2 * p + side + 1], a.n_rows);
@@ -744,7 +630,7 @@ __global__ __launch_bounds__(kThreads) void k_pairs(PairArgs a, const Stat *__re
                 const float w = a.weight ? a.weight[r] : 1.f;
                 const float gr = w == 0.f ? 0.f : (float)((double)w * (side ? -g : g));
                 if (fin) fin[r].g = gr;
-                else grad[r] = RowGrad{gr, 0.f};
+                else g_row[r] = gr;
             }
         }
     }
@@ -897,52 +783,248 @@ __global__ __launch_bounds__(kThreads) void k_grad(Rows q, int chunks, int per, 
     }
 }
 
-struct GradArgs {
-    const Stat *stat;              // {m, s, u, .} per (row, segment), or null: lse and entropy are given
-    const float *lse, *entropy;
-    const RowGrad *grad;           // per row, or null: g_logp and g_entropy
-    const float *g_logp, *g_entropy;
+// ------------------------------------------------------------------------------------------------
+// Heads of several segments, up to 4,096 columns.  A wave owns up to 64 consecutive rows, staged in LDS
+// as fp32; `lanes` lanes share a (row, segment) item.  Everything a row needs stays in its wave, so there
+// are no barriers between the steps: stage, sums of every item, a lane a row for the objective, gradients
+// of every item in place, write back.
+// ------------------------------------------------------------------------------------------------
+enum TypesMode : int { kTypesLogp, kTypesDiff, kTypesLoss, kTypesGradLse, kTypesGradPairs };
+
+constexpr int kTypesItems = 256;  // (row, segment) items of a wave at most
+constexpr int kTypesTile = 2048;  // columns of a wave's rows at most, or one row
+
+struct TypesShape {
+    int rows, lanes;      // rows of a wave, lanes of an item
+    uint32_t magic;       // ceil(2^32 / a): e / a = umulhi(e, magic) for the tile's e
+    int tile, bytes;      // floats of a wave's tile, bytes of a wave's LDS (a multiple of 16)
+};
+
+struct Item {
+    double lp;
+    float m, l2s, H, pad;  // m = -inf: an empty segment
+};
+
+struct TypesIO {
+    float *logp, *entropy, *lse;                            // outputs (kTypesLogp; kTypesLoss: logp)
+    const float *logp_ref;                                  // kTypesDiff
+    double *diff;                                           // [row] weight (logp - logp_ref)
+    float2 *norm;                                           // [row][segment] {m, log2 s}: out of kTypesDiff, into kTypesGradPairs
+    LossArgs loss;                                          // kTypesLoss
+    double *terms;                                          // [workgroup][3]
+    const float *in_lse, *in_entropy, *g_logp, *g_entropy;  // kTypesGradLse
+    const float *g_row;                                     // kTypesGradPairs
+    float *loss_out;                                        // kTypesGradPairs: summed by the launch's last workgroup
+    const double *pair_terms;
+    int n_pairs;
     void *dz;
     int64_t ld_d;
 };
 
+__device__ __forceinline__ void wave_sync() {  // LDS serves a wave's accesses in order
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// max / sum over groups of `lanes` consecutive lanes, in every lane of the group
+template <typename Op>
+__device__ __forceinline__ float group_reduce(float x, int lanes, float none, Op op) {
+    if (lanes == 64) return lanes_reduce<64>(x, none, op);
+    for (int o = lanes / 2; o > 0; o >>= 1) x = op(x, __shfl_xor(x, o));
+    return x;
+}
+
 template <typename T>
-__global__ __launch_bounds__(kThreads) void k_row_grad(Rows q, GradArgs a) {
-    for (int64_t r = blockIdx.x; r < q.M; r += gridDim.x) {
-        if (q.seq_ptr && (r < clamp_row(q.seq_ptr[0], q.M) || r >= clamp_row(q.seq_ptr[q.n_seq], q.M))) continue;
-        const T *z = static_cast<const T *>(q.z) + r * q.ld;
-        T *dz = static_cast<T *>(a.dz) + r * a.ld_d;
-        const float gl = a.grad ? a.grad[r].g_logp : a.g_logp[r];
-        const float ge = a.grad ? a.grad[r].g_ent : a.g_entropy ? a.g_entropy[r] : 0.f;
-        for (int g = 0; g < q.n_seg; ++g) {
-            const int lo = q.off[g], hi = q.off[g + 1];
-            const int act = min(max(q.act[r * q.n_seg + g], lo), hi - 1);
-            float m = 0.f, rest = 0.f, H = 0.f;  // log-sum-exp m + rest
-            bool empty = gl == 0.f && ge == 0.f;
-            if (a.stat) {
-                if (!empty) {
-                    const Stat t = a.stat[r * q.n_seg + g];
-                    empty = t.s == 0.f;
-                    m = t.m;
-                    rest = (float)log((double)t.s);
-                    H = (float)stat_entropy(t);
-                }
-            } else if (!empty) {
-                m = a.lse[(r * q.n_seg + g) * 2];
-                rest = a.lse[(r * q.n_seg + g) * 2 + 1];
-                empty = m == -INFINITY;
-                if (ge != 0.f) H = a.entropy[r * q.n_seg + g];
+__device__ __forceinline__ void load_tile(const T *z, int64_t ld, int a, int n, uint32_t magic, int head, float *zs, int lane) {
+    constexpr int N = kVec<T>;
+    const int total = n * a;
+    if (ld == a) {  // one run of columns: vectors behind the first aligned one, which zs was placed for
+        if (lane < head && lane < total) zs[lane] = to_f32(z[lane]);
+        const int full = max(total - head, 0) / N;
+        for (int v = lane; v < full; v += 64) {
+            float x[N];
+            unpack(reinterpret_cast<const uint4 *>(z + head)[v], x);
+            float4 *d = reinterpret_cast<float4 *>(zs + head + v * N);
+#pragma unroll
+            for (int i = 0; i < N / 4; ++i) d[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+        }
+        const int e = head + full * N + lane;
+        if (e < total) zs[e] = to_f32(z[e]);
+        return;
+    }
+#pragma unroll 4
+    for (int e = lane; e < total; e += 64) {
+        const int r = (int)__umulhi((uint32_t)e, magic);
+        zs[e] = to_f32(z[r * ld + (e - r * a)]);
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void store_tile(T *dz, int64_t ld, int a, int n, uint32_t magic, int head, const float *zs, int lane) {
+    constexpr int N = kVec<T>;
+    const int total = n * a;
+    const int mis = (int)(reinterpret_cast<uintptr_t>(dz) / sizeof(T)) & (N - 1);
+    if (ld == a && (mis ? N - mis : 0) == head) {
+        if (lane < head && lane < total) store(dz + lane, zs[lane]);
+        const int full = max(total - head, 0) / N;
+        for (int v = lane; v < full; v += 64) {
+            float x[N];
+            const float4 *s = reinterpret_cast<const float4 *>(zs + head + v * N);
+#pragma unroll
+            for (int i = 0; i < N / 4; ++i) {
+                const float4 f = s[i];
+                x[4 * i] = f.x, x[4 * i + 1] = f.y, x[4 * i + 2] = f.z, x[4 * i + 3] = f.w;
             }
-            for (int i = lo + (int)threadIdx.x; i < hi; i += kThreads) {
-                float d = 0.f;
-                if (!empty) {
-                    const float ls = (to_f32(z[i]) - m) - rest;
-                    const float p = expf(ls);
-                    d = gl * ((i == act ? 1.f : 0.f) - p);
-                    if (ge != 0.f) d -= ge * p * (fmaxf(ls, -1000.f) + H);
+            reinterpret_cast<uint4 *>(dz + head)[v] = pack(x);
+        }
+        const int e = head + full * N + lane;
+        if (e < total) store(dz + e, zs[e]);
+        return;
+    }
+#pragma unroll 4
+    for (int e = lane; e < total; e += 64) {
+        const int r = (int)__umulhi((uint32_t)e, magic);
+        store(dz + r * ld + (e - r * a), zs[e]);
+    }
+}
+
+template <typename T, int MODE>
+__global__ __launch_bounds__(kThreads) void k_types(Rows q, TypesShape sh, TypesIO io) {
+    constexpr int N = kVec<T>;
+    constexpr bool kGradOnly = MODE == kTypesGradLse || MODE == kTypesGradPairs;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    __shared__ int off[HARL_SELECT_MAX_SEGMENTS + 1];
+    if (MODE == kTypesGradPairs && io.loss_out && blockIdx.x == gridDim.x - 1) {
+        pairs_sum(io.pair_terms, io.n_pairs, io.loss_out);
+        return;
+    }
+    const unsigned groups = gridDim.x - (MODE == kTypesGradPairs && io.loss_out ? 1 : 0);
+    if (threadIdx.x <= (unsigned)q.n_seg) off[threadIdx.x] = q.off[threadIdx.x];
+    __syncthreads();
+    const int wv = threadIdx.x / 64, lane = threadIdx.x % 64, ns = q.n_seg, a = q.a;
+    const int items_max = sh.rows * ns;
+    char *mine = smem + wv * sh.bytes;
+    float *tile = reinterpret_cast<float *>(mine);
+    Item *item = reinterpret_cast<Item *>(mine + (size_t)sh.tile * 4);
+    float2 *row = reinterpret_cast<float2 *>(item + items_max);  // a row's gradients of log-probability and entropy
+    const int lo = q.seq_ptr ? clamp_row(q.seq_ptr[0], q.M) : 0, hi = q.seq_ptr ? clamp_row(q.seq_ptr[q.n_seq], q.M) : q.M;
+    const int L = sh.lanes, gl = lane % L, g0 = lane / L, gn = 64 / L;
+    double acc[3] = {0.0, 0.0, 0.0};
+    for (int64_t r0 = lo + ((int64_t)blockIdx.x * 4 + wv) * sh.rows; r0 < hi; r0 += (int64_t)groups * 4 * sh.rows) {
+        const int n = (int)min((int64_t)sh.rows, hi - r0), items = n * ns;
+        const T *z = static_cast<const T *>(q.z) + r0 * q.ld;
+        const int mis = (int)(reinterpret_cast<uintptr_t>(z) / sizeof(T)) & (N - 1), head = mis ? N - mis : 0;
+        float *zs = tile + ((4 - head) & 3);
+        load_tile<T>(z, q.ld, a, n, sh.magic, head, zs, lane);
+        wave_sync();
+        if (!kGradOnly) {
+            for (int p = g0; p < items; p += gn) {
+                const int r = p / ns, s = p - r * ns, i1 = off[s + 1];
+                const float *x = zs + r * a;
+                float m = -INFINITY;
+                for (int i = off[s] + gl; i < i1; i += L) m = max_nan(m, x[i]);
+                m = group_reduce(m, L, -INFINITY, [](float b, float c) { return max_nan(b, c); });
+                const float ms = shift_of(m);
+                Sums sum{m, 0.f, 0.f};
+                for (int i = off[s] + gl; i < i1; i += L) {
+                    const float y = fmaxf((x[i] - ms) * kLog2e, kYMin), e = exp2_hw(y);
+                    sum.s += e;
+                    sum.u = fmaf(e, y, sum.u);
                 }
-                store(dz + i, d);
+                const auto add = [](float b, float c) { return b + c; };
+                sum.s = group_reduce(sum.s, L, 0.f, add);
+                sum.u = group_reduce(sum.u, L, 0.f, add);
+                if (!(m < INFINITY)) sum.s = sum.u = __builtin_nanf("");
+                if (gl != 0) continue;
+                const int64_t e = (r0 + r) * ns + s;
+                const float zact = x[min(max(q.act[e], off[s]), i1 - 1)];
+                Item it{};
+                it.m = sum.s == 0.f ? -INFINITY : m;
+                it.l2s = __builtin_amdgcn_logf(sum.s);
+                it.lp = log_prob(sum, zact);
+                if (MODE == kTypesLoss) it.H = (float)entropy_of(sum);
+                if (MODE == kTypesDiff) io.norm[e] = make_float2(it.m, it.l2s);
+                if (MODE == kTypesLogp && io.entropy) io.entropy[e] = (float)entropy_of(sum);
+                if (MODE == kTypesLogp && io.lse) {
+                    io.lse[2 * e] = m;
+                    io.lse[2 * e + 1] = sum.s == 0.f ? 0.f : (float)log_sum(sum);
+                }
+                item[p] = it;
             }
+            wave_sync();
+        }
+        if (lane < n) {
+            const int64_t r = r0 + lane;
+            double lp = 0.0, H = 0.0;
+            if (!kGradOnly)
+                for (int s = 0; s < ns; ++s) {
+                    lp += item[lane * ns + s].lp;
+                    H += (double)item[lane * ns + s].H;
+                }
+            float2 g = make_float2(0.f, 0.f);
+            if (MODE == kTypesLogp) io.logp[r] = (float)lp;
+            if (MODE == kTypesDiff) {
+                const float w = q.weight ? q.weight[r] : 1.f;
+                io.diff[r] = w == 0.f ? 0.0 : (double)w * (lp - (io.logp_ref ? (double)io.logp_ref[r] : 0.0));
+            }
+            if (MODE == kTypesLoss) {
+                const float w = io.loss.weight ? io.loss.weight[r] : io.loss.inv_m;
+                if (w != 0.f) {
+                    float surrogate, kl;
+                    loss_grad(io.loss, w, io.loss.logp_old[r], io.loss.logp_ref ? io.loss.logp_ref[r] : 0.f, io.loss.adv[r], (float)lp,
+                              g.x, g.y, surrogate, kl);
+                    acc[0] -= (double)w * (double)surrogate;
+                    acc[1] += (double)w * (double)kl;
+                    acc[2] += (double)w * H;
+                }
+                if (io.logp) io.logp[r] = w != 0.f ? (float)lp : 0.f;
+            }
+            if (MODE == kTypesGradLse) g = make_float2(io.g_logp[r], io.g_entropy ? io.g_entropy[r] : 0.f);
+            if (MODE == kTypesGradPairs) g.x = io.g_row[r];
+            row[lane] = g;
+        }
+        wave_sync();
+        if (MODE == kTypesLogp || MODE == kTypesDiff || !io.dz) continue;
+        for (int p = g0; p < items; p += gn) {
+            const int r = p / ns, s = p - r * ns, i1 = off[s + 1];
+            const int64_t e = (r0 + r) * ns + s;
+            float *x = zs + r * a;
+            const float2 g = row[r];
+            float m, l2s, H = 0.f;
+            if (MODE == kTypesLoss) {
+                m = item[p].m, l2s = item[p].l2s, H = item[p].H;
+            } else if (MODE == kTypesGradPairs) {
+                m = -INFINITY, l2s = 0.f;
+                if (g.x != 0.f) m = io.norm[e].x, l2s = io.norm[e].y;
+            } else {
+                m = io.in_lse[2 * e], l2s = io.in_lse[2 * e + 1] * kLog2e;
+                if (g.y != 0.f) H = io.in_entropy[e];
+            }
+            const RowCoef k = coef_of(m, m == -INFINITY ? 0.f : 1.f, l2s, H, g.x, g.y);
+            if (k.zero != 0.f) {
+                for (int i = off[s] + gl; i < i1; i += L) x[i] = 0.f;
+                continue;
+            }
+            const int act = min(max(q.act[e], off[s]), i1 - 1);
+            for (int i = off[s] + gl; i < i1; i += L) x[i] = grad_any(k, x[i]) + (i == act ? k.g : 0.f);
+        }
+        wave_sync();
+        store_tile<T>(static_cast<T *>(io.dz) + r0 * io.ld_d, io.ld_d, a, n, sh.magic, head, zs, lane);
+        wave_sync();
+    }
+    if (MODE == kTypesLoss) {
+        __shared__ double part[4][3];
+#pragma unroll
+        for (int c = 0; c < 3; ++c) {
+            double v = acc[c];
+            for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+            if (lane == 0) part[wv][c] = v;
+        }
+        __syncthreads();
+        if (threadIdx.x < 3) {
+            double v = 0.0;
+            for (int w = 0; w < 4; ++w) v += part[w][threadIdx.x];
+            io.terms[(int64_t)blockIdx.x * 3 + threadIdx.x] = v;
         }
     }
 }
@@ -960,24 +1042,6 @@ Rows rows_of(const harl_policy_head *h, const void *z, int64_t ld, int32_t M, co
 }
 
 unsigned grid_for(int64_t items) { return (unsigned)std::min<int64_t>(std::max<int64_t>(items, 1), kMaxGrid); }
-
-int launch_stats(const harl_policy_head *h, const Rows &q, Stat *stat, hipStream_t stream) {
-    if (h->dtype == HARL_BF16)
-        hipLaunchKernelGGL(k_row_stats<uint16_t>, dim3(grid_for(q.M)), dim3(kThreads), 0, stream, q, stat);
-    else
-        hipLaunchKernelGGL(k_row_stats<float>, dim3(grid_for(q.M)), dim3(kThreads), 0, stream, q, stat);
-    HARL_HIP_CHECK(hipGetLastError());
-    return HARL_OK;
-}
-
-int launch_grad(const harl_policy_head *h, const Rows &q, const GradArgs &a, hipStream_t stream) {
-    if (h->dtype == HARL_BF16)
-        hipLaunchKernelGGL(k_row_grad<uint16_t>, dim3(grid_for(q.M)), dim3(kThreads), 0, stream, q, a);
-    else
-        hipLaunchKernelGGL(k_row_grad<float>, dim3(grid_for(q.M)), dim3(kThreads), 0, stream, q, a);
-    HARL_HIP_CHECK(hipGetLastError());
-    return HARL_OK;
-}
 
 // ---- launch shapes of one-segment heads ----
 int vec_of(const harl_policy_head *h) { return h->dtype == HARL_BF16 ? 8 : 4; }
@@ -1048,42 +1112,91 @@ unsigned launch_loss(const Rows &q, const LossArgs &a, const LossOut &o, hipStre
     return launch_loss_as<T, 1024, 16>(q, a, o, stream);
 }
 
-// The workspace: statistics per (row, segment) or (row, chunk), per-row gradients, loss terms.
+// ---- launch shapes of heads of several segments ----
+TypesShape types_shape(const harl_policy_head *h, int32_t M) {
+    TypesShape s{};
+    int longest = 1;
+    for (int i = 0; i < h->n_seg; ++i) longest = std::max(longest, h->seg_offsets[i + 1] - h->seg_offsets[i]);
+    // enough waves to fill the machine (8 a SIMD), rows enough to keep a wave's loads wide
+    const int64_t most = std::max<int64_t>(1, std::min<int64_t>({64, kTypesItems / h->n_seg, kTypesTile / h->a}));
+    s.rows = (int)std::max<int64_t>(1, std::min<int64_t>(most, ceil_div(M, 8192)));
+    // lanes for about 16 columns each of the longest segment, more where a wave has too few items for its lanes
+    int lanes = 1;
+    while (lanes < 64 && lanes * 16 < longest) lanes *= 2;
+    while (lanes < 64 && lanes < longest && lanes * 2 * s.rows * h->n_seg <= 64) lanes *= 2;
+    s.lanes = lanes;
+    s.magic = (uint32_t)((((uint64_t)1 << 32) + h->a - 1) / h->a);
+    s.tile = (int)round_up((int64_t)s.rows * h->a + 4, 4);
+    s.bytes = s.tile * 4 + s.rows * h->n_seg * (int)sizeof(Item) + (int)round_up(s.rows * 8, 16);
+    return s;
+}
+
+template <typename T, int MODE>
+int launch_types_as(const harl_policy_head *h, const Rows &q, const TypesIO &io, unsigned grid, unsigned extra, const TypesShape &s,
+                    hipStream_t stream) {
+    const size_t lds = 4 * (size_t)s.bytes;
+    if (const int rc = ensure_dynamic_lds(reinterpret_cast<const void *>(k_types<T, MODE>), lds)) return rc;
+    hipLaunchKernelGGL((k_types<T, MODE>), dim3(grid + extra), dim3(kThreads), lds, stream, q, s, io);
+    HARL_HIP_CHECK(hipGetLastError());
+    return HARL_OK;
+}
+
+unsigned types_grid(const TypesShape &s, int32_t M) {
+    return (unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div(M, 4 * (int64_t)s.rows), kLossGrid));
+}
+
+template <int MODE>
+int launch_types(const harl_policy_head *h, const Rows &q, const TypesIO &io, hipStream_t stream) {
+    const TypesShape s = types_shape(h, q.M);
+    const unsigned grid = types_grid(s, q.M), extra = MODE == kTypesGradPairs && io.loss_out ? 1 : 0;
+    return h->dtype == HARL_BF16 ? launch_types_as<uint16_t, MODE>(h, q, io, grid, extra, s, stream)
+                                 : launch_types_as<float, MODE>(h, q, io, grid, extra, s, stream);
+}
+
+// The workspace: statistics per (row, chunk), what the preference loss keeps of a row, loss terms.
 struct Ws {
     Stat *stat;
-    RowGrad *grad;
     RowFin *fin;
+    double *diff;
+    float2 *norm;
+    float *g_row;
     double *terms;
     size_t bytes;
 };
 
-Ws ws_layout(int64_t n_stat, int64_t n_grad, int64_t n_fin, int64_t n_terms, char *base) {
+struct WsCounts {
+    int64_t stat, fin, rows, norm, terms;
+};
+
+Ws ws_layout(const WsCounts &n, char *base) {
     Ws w{};
     int64_t off = 0;
     auto take = [&](int64_t bytes) {
         char *p = base ? base + off : nullptr;
-        off += round_up(std::max<int64_t>(bytes, 1), 256);
+        off += round_up(bytes, 256);
         return p;
     };
-    w.stat = reinterpret_cast<Stat *>(take(n_stat * (int64_t)sizeof(Stat)));
-    w.grad = reinterpret_cast<RowGrad *>(take(n_grad * (int64_t)sizeof(RowGrad)));
-    w.fin = reinterpret_cast<RowFin *>(take(n_fin * (int64_t)sizeof(RowFin)));
-    w.terms = reinterpret_cast<double *>(take(n_terms * 8));
-    w.bytes = (size_t)off;
+    w.stat = reinterpret_cast<Stat *>(take(n.stat * (int64_t)sizeof(Stat)));
+    w.fin = reinterpret_cast<RowFin *>(take(n.fin * (int64_t)sizeof(RowFin)));
+    w.diff = reinterpret_cast<double *>(take(n.rows * 8));
+    w.norm = reinterpret_cast<float2 *>(take(n.norm * 8));
+    w.g_row = reinterpret_cast<float *>(take(n.rows * 4));
+    w.terms = reinterpret_cast<double *>(take(n.terms * 8));
+    w.bytes = (size_t)std::max<int64_t>(off, 256);
     return w;
 }
 
-// Few rows in chunks: at most rows + kSplitItems items.
+// Rows in chunks: at most rows + kSplitItems items, and none in chunks from kSplitItems rows on.
 Ws logp_ws(const harl_policy_head *h, int64_t M, char *base) {
-    return h->n_seg == 1 ? ws_layout(std::min<int64_t>(M, kSplitItems) + kSplitItems, 0, 0, 0, base)
-                         : ws_layout(M * h->n_seg, 0, 0, 0, base);
+    return ws_layout(WsCounts{h->n_seg == 1 ? std::min<int64_t>(M, kSplitItems) + kSplitItems : 0, 0, 0, 0, 0}, base);
 }
 Ws loss_ws(const harl_policy_head *h, int64_t M, char *base) {
-    return h->n_seg == 1 ? ws_layout(std::min<int64_t>(M, kSplitItems) + kSplitItems, 0, 0, 3 * std::min<int64_t>(M, kLossGrid), base)
-                         : ws_layout(M * h->n_seg, M, 0, 3 * M, base);
+    return ws_layout(WsCounts{h->n_seg == 1 ? std::min<int64_t>(M, kSplitItems) + kSplitItems : 0, 0, 0, 0,
+                              3 * std::min<int64_t>(M, kLossGrid)}, base);
 }
 Ws preference_ws(const harl_policy_head *h, int64_t rows, int64_t pairs, char *base) {
-    return h->n_seg == 1 ? ws_layout(rows + kSplitItems, 0, rows, 4 * pairs, base) : ws_layout(rows * h->n_seg, rows, 0, 4 * pairs, base);
+    return ws_layout(h->n_seg == 1 ? WsCounts{rows + kSplitItems, rows, 0, 0, 4 * pairs}
+                                   : WsCounts{0, 0, rows, rows * h->n_seg, 4 * pairs}, base);
 }
 
 }  // namespace
@@ -1100,18 +1213,18 @@ int policy_logp_launch(const harl_policy_head *head, const void *logits, int64_t
                        float *logp, float *entropy, float *lse, void *ws, hipStream_t stream) {
     const Ws w = logp_ws(head, M, static_cast<char *>(ws));
     const Rows q = rows_of(head, logits, ld, M, actions);
-    if (head->n_seg == 1) {
-        const int chunks = chunks_for(head, M);
-        const StatOut o{w.stat, logp, entropy, lse};
-        if (chunks == 1) return launch_wide_stats<kLogp>(head, q, 1, o, stream);
-        if (const int rc = launch_wide_stats<kPartial>(head, q, chunks, o, stream)) return rc;
-        hipLaunchKernelGGL(k_logp_join, dim3(grid_for(ceil_div(M, 64))), dim3(64), 0, stream, w.stat, M, chunks, o);
-        HARL_HIP_CHECK(hipGetLastError());
-        return HARL_OK;
+    if (head->n_seg > 1) {
+        TypesIO io{};
+        io.logp = logp;
+        io.entropy = entropy;
+        io.lse = lse;
+        return launch_types<kTypesLogp>(head, q, io, stream);
     }
-    if (const int rc = launch_stats(head, q, w.stat, stream)) return rc;
-    hipLaunchKernelGGL(k_logp_rows, dim3(grid_for(ceil_div(M, kThreads))), dim3(kThreads), 0, stream, w.stat, M,
-                       head->n_seg, logp, entropy, lse);
+    const int chunks = chunks_for(head, M);
+    const StatOut o{w.stat, logp, entropy, lse};
+    if (chunks == 1) return launch_wide_stats<kLogp>(head, q, 1, o, stream);
+    if (const int rc = launch_wide_stats<kPartial>(head, q, chunks, o, stream)) return rc;
+    hipLaunchKernelGGL(k_logp_join, dim3(grid_for(ceil_div(M, 64))), dim3(64), 0, stream, w.stat, M, chunks, o);
     HARL_HIP_CHECK(hipGetLastError());
     return HARL_OK;
 }
@@ -1120,24 +1233,24 @@ int policy_logp_grad_launch(const harl_policy_head *head, const void *logits, in
                             const int32_t *actions, const float *lse, const float *entropy, const float *g_logp,
                             const float *g_entropy, void *dlogits, int64_t ld_d, hipStream_t stream) {
     const Rows q = rows_of(head, logits, ld, M, actions);
-    if (head->n_seg == 1) {
-        GradSrc a{};
-        a.lse = lse;
-        a.entropy = entropy;
-        a.g_logp = g_logp;
-        a.g_entropy = g_entropy;
-        a.dz = dlogits;
-        a.ld_d = ld_d;
-        return launch_wide_grad<kFromLse>(head, q, a, stream);
+    if (head->n_seg > 1) {
+        TypesIO io{};
+        io.in_lse = lse;
+        io.in_entropy = entropy;
+        io.g_logp = g_logp;
+        io.g_entropy = g_entropy;
+        io.dz = dlogits;
+        io.ld_d = ld_d;
+        return launch_types<kTypesGradLse>(head, q, io, stream);
     }
-    GradArgs a{};
+    GradSrc a{};
     a.lse = lse;
     a.entropy = entropy;
     a.g_logp = g_logp;
     a.g_entropy = g_entropy;
     a.dz = dlogits;
     a.ld_d = ld_d;
-    return launch_grad(head, q, a, stream);
+    return launch_wide_grad<kFromLse>(head, q, a, stream);
 }
 
 int policy_loss_launch(const harl_policy_head *head, const harl_policy_loss_config *cfg, const void *logits, int64_t ld,
@@ -1148,8 +1261,17 @@ int policy_loss_launch(const harl_policy_head *head, const harl_policy_loss_conf
     Rows q = rows_of(head, logits, ld, M, actions);
     q.weight = weight;
     const LossArgs a{logp_old, logp_ref, adv, weight, cfg->clip_low, cfg->clip_high, cfg->w_kl, cfg->w_entropy, 1.f / (float)M};
-    int64_t n_terms = M;
-    if (head->n_seg == 1) {
+    int64_t n_terms = 0;
+    if (head->n_seg > 1) {
+        TypesIO io{};
+        io.loss = a;
+        io.logp = logp;
+        io.terms = w.terms;
+        io.dz = dlogits;
+        io.ld_d = ld_d;
+        if (const int rc = launch_types<kTypesLoss>(head, q, io, stream)) return rc;
+        n_terms = types_grid(types_shape(head, M), M);
+    } else {
         const int chunks = chunks_for(head, M);
         if (chunks > 1) {
             const StatOut o{w.stat, nullptr, nullptr, nullptr};
@@ -1167,23 +1289,11 @@ int policy_loss_launch(const harl_policy_head *head, const harl_policy_loss_conf
         const LossOut o{dlogits, ld_d, logp, w.terms};
         n_terms = head->dtype == HARL_BF16 ? launch_loss<uint16_t>(q, a, o, stream) : launch_loss<float>(q, a, o, stream);
         HARL_HIP_CHECK(hipGetLastError());
-    } else {
-        if (const int rc = launch_stats(head, q, w.stat, stream)) return rc;
-        hipLaunchKernelGGL(k_loss_rows, dim3(grid_for(ceil_div(M, kThreads))), dim3(kThreads), 0, stream, a, w.stat, M,
-                           head->n_seg, w.grad, w.terms, logp);
-        HARL_HIP_CHECK(hipGetLastError());
     }
-    if (loss) {
-        hipLaunchKernelGGL(k_loss_sum, dim3(1), dim3(kThreads), 0, stream, w.terms, n_terms, cfg->w_kl, cfg->w_entropy, loss);
-        HARL_HIP_CHECK(hipGetLastError());
-    }
-    if (!dlogits || head->n_seg == 1) return HARL_OK;
-    GradArgs g{};
-    g.stat = w.stat;
-    g.grad = w.grad;
-    g.dz = dlogits;
-    g.ld_d = ld_d;
-    return launch_grad(head, q, g, stream);
+    if (!loss) return HARL_OK;
+    hipLaunchKernelGGL(k_loss_sum, dim3(1), dim3(kThreads), 0, stream, w.terms, n_terms, cfg->w_kl, cfg->w_entropy, loss);
+    HARL_HIP_CHECK(hipGetLastError());
+    return HARL_OK;
 }
 
 int preference_loss_launch(const harl_policy_head *head, const harl_preference_config *cfg, const void *logits,
@@ -1195,18 +1305,34 @@ int preference_loss_launch(const harl_policy_head *head, const harl_preference_c
     q.weight = weight;
     q.seq_ptr = seq_ptr;
     q.n_seq = 2 * n_pairs;
-    const bool grad = dlogits && n_rows > 0, wide = head->n_seg == 1;
-    const int chunks = wide && n_rows > 0 ? chunks_for(head, n_rows) : 1;
-    if (n_rows > 0) {
+    const bool grad = dlogits && n_rows > 0, types = head->n_seg > 1;
+    const int chunks = !types && n_rows > 0 ? chunks_for(head, n_rows) : 1;
+    if (n_rows > 0 && types) {
+        TypesIO io{};
+        io.logp_ref = logp_ref;
+        io.diff = w.diff;
+        io.norm = w.norm;
+        if (const int rc = launch_types<kTypesDiff>(head, q, io, stream)) return rc;
+    } else if (n_rows > 0) {
         const StatOut o{w.stat, nullptr, nullptr, nullptr};
-        if (const int rc = wide ? launch_wide_stats<kPartial>(head, q, chunks, o, stream) : launch_stats(head, q, w.stat, stream))
-            return rc;
+        if (const int rc = launch_wide_stats<kPartial>(head, q, chunks, o, stream)) return rc;
     }
-    const PairArgs a{logp_ref, weight, seq_ptr, n_rows, head->n_seg, chunks, n_pairs, cfg->beta, cfg->smoothing};
-    hipLaunchKernelGGL(k_pairs, dim3(grid_for(n_pairs)), dim3(kThreads), 0, stream, a, w.stat, grad && wide ? w.fin : nullptr,
-                       grad && !wide ? w.grad : nullptr, w.terms, ratio);
+    const PairArgs a{logp_ref, weight, seq_ptr, n_rows, chunks, n_pairs, cfg->beta, cfg->smoothing};
+    hipLaunchKernelGGL(k_pairs, dim3(grid_for(n_pairs)), dim3(kThreads), 0, stream, a, w.stat, types ? w.diff : nullptr,
+                       grad && !types ? w.fin : nullptr, grad && types ? w.g_row : nullptr, w.terms, ratio);
     HARL_HIP_CHECK(hipGetLastError());
-    if (grad && wide) {
+    if (grad && types) {
+        TypesIO io{};
+        io.norm = w.norm;
+        io.g_row = w.g_row;
+        io.loss_out = loss;
+        io.pair_terms = w.terms;
+        io.n_pairs = n_pairs;
+        io.dz = dlogits;
+        io.ld_d = ld_d;
+        return launch_types<kTypesGradPairs>(head, q, io, stream);
+    }
+    if (grad) {
         GradSrc g{};
         g.fin = w.fin;
         g.loss_out = loss;
@@ -1216,17 +1342,10 @@ int preference_loss_launch(const harl_policy_head *head, const harl_preference_c
         g.ld_d = ld_d;
         return launch_wide_grad<kFromFin>(head, q, g, stream);
     }
-    if (loss) {
-        hipLaunchKernelGGL(k_pairs_sum, dim3(1), dim3(kThreads), 0, stream, w.terms, n_pairs, loss);
-        HARL_HIP_CHECK(hipGetLastError());
-    }
-    if (!grad) return HARL_OK;
-    GradArgs g{};
-    g.stat = w.stat;
-    g.grad = w.grad;
-    g.dz = dlogits;
-    g.ld_d = ld_d;
-    return launch_grad(head, q, g, stream);
+    if (!loss) return HARL_OK;
+    hipLaunchKernelGGL(k_pairs_sum, dim3(1), dim3(kThreads), 0, stream, w.terms, n_pairs, loss);
+    HARL_HIP_CHECK(hipGetLastError());
+    return HARL_OK;
 }
 
 }  // namespace harl
