@@ -251,6 +251,17 @@ __device__ __forceinline__ double entropy_of(const Sums &q) {
     return q.s == 0.f ? 0.0 : log_sum(q) - kLn2d * (double)q.u / (double)q.s;
 }
 
+// The same in fp32, for what is rounded to fp32 next: log s and its error of log2 e.
+struct LogSum {
+    float l2s, ls, mean_y;
+};
+__device__ __forceinline__ LogSum log_sum_f32(const Sums &q) {
+    const float l2s = __builtin_amdgcn_logf(q.s), mean_y = q.u / q.s;
+    return LogSum{l2s, fmaf(l2s, kLn2, (float)(kLog2eRest * kLn2d * kLn2d) * mean_y), mean_y};
+}
+__device__ __forceinline__ float log_prob_f32(const Sums &q, const LogSum &l, float zact) { return q.s == 0.f ? 0.f : (zact - q.m) - l.ls; }
+__device__ __forceinline__ float entropy_f32(const Sums &q, const LogSum &l) { return q.s == 0.f ? 0.f : l.ls - kLn2 * l.mean_y; }
+
 // What the gradient of a row is made of: dz_i = -p_i (g + h (y_i + shift of H)) and g more at the action,
 // p = 2^y, y = (z - m) log2 e - log2 s.  Written as p (c + e y): c = -(g_logp + g_H H), e = -g_H ln 2.
 struct RowCoef {
@@ -316,6 +327,16 @@ struct StatOut {
     float *logp, *entropy, *lse;
 };
 
+__device__ __forceinline__ void put_logp(const StatOut &o, int64_t r, const Sums &q, float zact) {
+    const LogSum l = log_sum_f32(q);
+    o.logp[r] = log_prob_f32(q, l, zact);
+    if (o.entropy) o.entropy[r] = entropy_f32(q, l);
+    if (o.lse) {
+        o.lse[2 * r] = q.m;
+        o.lse[2 * r + 1] = q.s == 0.f ? 0.f : l.ls;
+    }
+}
+
 template <typename T, int TPR, int NV, int OUT>
 __global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void k_stats(Rows q, int chunks, int per, StatOut o) {
     constexpr int WG = TPR < kThreads ? kThreads : TPR, N = kVec<T>;
@@ -355,43 +376,43 @@ __global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void k_stats(Rows 
             if (OUT == kPartial) {
                 o.stat[it] = Stat{sum.m, sum.s, sum.u, zact};
             } else {
-                o.logp[r] = (float)log_prob(sum, zact);
-                if (o.entropy) o.entropy[r] = (float)entropy_of(sum);
-                if (o.lse) {
-                    o.lse[2 * (int64_t)r] = sum.m;
-                    o.lse[2 * (int64_t)r + 1] = sum.s == 0.f ? 0.f : (float)log_sum(sum);
-                }
+                put_logp(o, r, sum, zact);
             }
         }
     }
 }
 
-// A row's sums from its chunks', by one thread in chunk order.
-__device__ __forceinline__ Sums join_chunks(const Stat *st, int chunks) {
-    Sums q{st[0].m, st[0].s, st[0].u};
-    if (chunks == 1) return q;
-    for (int c = 1; c < chunks; ++c) q.m = max_nan(q.m, st[c].m);
-    const float m = q.m, ms = shift_of(m);
-    q = Sums{m, 0.f, 0.f};
-    for (int c = 0; c < chunks; ++c) {
-        Sums x{st[c].m, st[c].s, st[c].u};
-        rescale(x, m, ms);
-        q.s += x.s;
-        q.u += x.u;
+// A row's sums from its chunks', by one thread in chunk order, eight loads in flight.
+__device__ __forceinline__ Sums join_chunks(const Stat *__restrict__ st, int chunks) {
+    if (chunks == 1) return Sums{st[0].m, st[0].s, st[0].u};
+    Sums q{-INFINITY, 0.f, 0.f};
+    for (int c = 0; c < chunks; c += 8) {
+        Stat x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = st[min(c + j, chunks - 1)];
+        float m = q.m;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) m = max_nan(m, x[j].m);
+        const float ms = shift_of(m);
+        rescale(q, m, ms);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            Sums y{x[j].m, x[j].s, x[j].u};
+            rescale(y, m, ms);
+            if (c + j < chunks) {
+                q.s += y.s;
+                q.u += y.u;
+            }
+        }
     }
-    if (!(m < INFINITY)) q.s = q.u = __builtin_nanf("");
+    if (!(q.m < INFINITY)) q.s = q.u = __builtin_nanf("");
     return q;
 }
 
 __global__ __launch_bounds__(64) void k_logp_join(const Stat *__restrict__ stat, int M, int chunks, StatOut o) {
     for (int64_t r = (int64_t)blockIdx.x * 64 + threadIdx.x; r < M; r += (int64_t)gridDim.x * 64) {
         const Sums sum = join_chunks(stat + r * chunks, chunks);
-        o.logp[r] = (float)log_prob(sum, stat[r * chunks].zact);
-        if (o.entropy) o.entropy[r] = (float)entropy_of(sum);
-        if (o.lse) {
-            o.lse[2 * r] = sum.m;
-            o.lse[2 * r + 1] = sum.s == 0.f ? 0.f : (float)log_sum(sum);
-        }
+        put_logp(o, r, sum, stat[r * chunks].zact);
     }
 }
 
@@ -518,11 +539,8 @@ __global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void k_loss(Rows q
             add_values<1>(sum, x);
         }
         sum = row_join<TPR>(sum, red, half);
-        const float l2s = __builtin_amdgcn_logf(sum.s);
-        const float mean_y = sum.u / sum.s;
-        const float lsum = fmaf(l2s, kLn2, (float)(kLog2eRest * kLn2d * kLn2d) * mean_y);
-        const float logp = sum.s == 0.f ? 0.f : (zact - sum.m) - lsum;
-        const float H = sum.s == 0.f ? 0.f : lsum - kLn2 * mean_y;
+        const LogSum l = log_sum_f32(sum);
+        const float logp = log_prob_f32(sum, l, zact), H = entropy_f32(sum, l);
         float gl, ge, surrogate, kl;
         loss_grad(a, w, old, ref, adv, logp, gl, ge, surrogate, kl);
         acc[0] -= (double)w * (double)surrogate;
@@ -530,7 +548,7 @@ __global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void k_loss(Rows q
         acc[2] += (double)w * (double)H;
         if (t == 0 && o.logp) o.logp[r] = logp;
         if (!GRAD) continue;
-        const RowCoef k = coef_of(sum.m, sum.s, l2s, H, gl, ge);
+        const RowCoef k = coef_of(sum.m, sum.s, l.l2s, H, gl, ge);
         if (k.zero != 0.f) {
             zero_row<T, TPR>(dz, q.a, t);
             continue;
@@ -578,41 +596,48 @@ struct PairArgs {
 __global__ __launch_bounds__(kThreads) void k_pairs(PairArgs a, const Stat *__restrict__ stat, const double *__restrict__ diff,
                                                     RowFin *__restrict__ fin, float *__restrict__ g_row,
                                                     double *__restrict__ terms, float *__restrict__ ratio) {
-    __shared__ double part[kThreads];
+    __shared__ double part[2][2][kThreads / 64];
+    int half = 0;
     for (int64_t p = blockIdx.x; p < a.n_pairs; p += gridDim.x) {
-        double R[2];
-        for (int side = 0; side < 2; ++side) {
-            const int lo = clamp_row(a.seq_ptr[2 * p + side], a.n_rows), hi = clamp_row(a.seq_ptr[2 * p + side + 1], a.n_rows);
-            double s = 0.0;
-            for (int64_t r = (int64_t)lo + threadIdx.x; r < hi; r += kThreads) {
+        // in order these are one run of rows, the rejected track's behind the preferred one's
+        const int lo = clamp_row(a.seq_ptr[2 * p], a.n_rows), mid = clamp_row(a.seq_ptr[2 * p + 1], a.n_rows);
+        const int hi = clamp_row(a.seq_ptr[2 * p + 2], a.n_rows);
+        double s[2] = {0.0, 0.0};
+        for (int64_t r = (int64_t)lo + threadIdx.x; r < hi; r += kThreads) {
+            double d;
+            if (diff) {
+                d = diff[r];
+            } else {
                 const float w = a.weight ? a.weight[r] : 1.f;
                 if (w == 0.f) continue;
-                if (diff) {
-                    s += diff[r];
-                    continue;
-                }
+                const float ref = a.logp_ref ? a.logp_ref[r] : 0.f;
                 const Sums q = join_chunks(stat + r * a.chunks, a.chunks);
-                const double lp = log_prob(q, stat[r * a.chunks].zact) - (a.logp_ref ? (double)a.logp_ref[r] : 0.0);
+                d = (double)w * (log_prob(q, stat[r * a.chunks].zact) - (double)ref);
                 if (fin) {
                     fin[r].m = q.s == 0.f ? -INFINITY : q.m;
-                    fin[r].l2s = (float)(log((double)q.s) * 1.4426950408889634);
+                    fin[r].l2s = __builtin_amdgcn_logf(q.s);
                 }
-                s += (double)w * lp;
             }
-            part[threadIdx.x] = s;
-            __syncthreads();
-            for (int h = kThreads / 2; h > 0; h >>= 1) {
-                if ((int)threadIdx.x < h) part[threadIdx.x] += part[threadIdx.x + h];
-                __syncthreads();
-            }
-            R[side] = part[0];
-            __syncthreads();
+            s[r >= mid ? 1 : 0] += d;
         }
+        for (int side = 0; side < 2; ++side) {
+            double v = s[side];
+            for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+            if (threadIdx.x % 64 == 0) part[half][side][threadIdx.x / 64] = v;
+        }
+        __syncthreads();
+        double R[2];
+        for (int side = 0; side < 2; ++side) {
+            R[side] = part[half][side][0];
+            for (int i = 1; i < kThreads / 64; ++i) R[side] += part[half][side][i];
+        }
+        half ^= 1;  // the next pair's sums go to the other half: one barrier a pair
         const double h = (double)a.beta * (R[0] - R[1]);
         // -log sigmoid(h) = log(1 + e^-|h|) + max(-h, 0); d/dh of the loss = smoothing - sigmoid(-h)
-        const double lose = log1p(exp(-fabs(h))) + (h < 0.0 ? -h : (h == h ? 0.0 : h));
-        const double down = h >= 0.0 ? exp(-h) / (1.0 + exp(-h)) : 1.0 / (1.0 + exp(h));
+        const double e = exp(-fabs(h));
+        const double down = (h >= 0.0 ? e : 1.0) / (1.0 + e);
         if (threadIdx.x == 0) {
+            const double lose = log1p(e) + (h < 0.0 ? -h : (h == h ? 0.0 : h));
             terms[p * 4] = a.smoothing != 0.f ? lose + (double)a.smoothing * h : lose;
             terms[p * 4 + 1] = lose;
             terms[p * 4 + 2] = h;
@@ -624,14 +649,11 @@ __global__ __launch_bounds__(kThreads) void k_pairs(PairArgs a, const Stat *__re
         }
         if (!fin && !g_row) continue;
         const double g = (double)a.beta * ((double)a.smoothing - down) / (double)a.n_pairs;
-        for (int side = 0; side < 2; ++side) {
-            const int lo = clamp_row(a.seq_ptr[2 * p + side], a.n_rows), hi = clamp_row(a.seq_ptr[2 * p + side + 1], a.n_rows);
-            for (int64_t r = (int64_t)lo + threadIdx.x; r < hi; r += kThreads) {
-                const float w = a.weight ? a.weight[r] : 1.f;
-                const float gr = w == 0.f ? 0.f : (float)((double)w * (side ? -g : g));
-                if (fin) fin[r].g = gr;
-                else g_row[r] = gr;
-            }
+        for (int64_t r = (int64_t)lo + threadIdx.x; r < hi; r += kThreads) {
+            const float w = a.weight ? a.weight[r] : 1.f;
+            const float gr = w == 0.f ? 0.f : (float)((double)w * (r >= mid ? -g : g));
+            if (fin) fin[r].g = gr;
+            else g_row[r] = gr;
         }
     }
 }
@@ -777,8 +799,8 @@ __global__ __launch_bounds__(kThreads) void k_grad(Rows q, int chunks, int per, 
             }
         }
         if (c == 0) {
-            const int i = parts.edge(t);
-            if (i >= 0) store(dz + i, k.zero != 0.f ? 0.f : grad_any(k, to_f32(z[i])) + (i == act ? k.g : 0.f));
+            const int e = parts.edge(t);
+            if (e >= 0) store(dz + e, k.zero != 0.f ? 0.f : grad_any(k, to_f32(z[e])) + (e == act ? k.g : 0.f));
         }
     }
 }
@@ -797,12 +819,14 @@ constexpr int kTypesTile = 2048;  // columns of a wave's rows at most, or one ro
 struct TypesShape {
     int rows, lanes;      // rows of a wave, lanes of an item
     uint32_t magic;       // ceil(2^32 / a): e / a = umulhi(e, magic) for the tile's e
+    int seg_magic;        // ceil(2^16 / n_seg): p / n_seg = p seg_magic >> 16 for a wave's items
     int tile, bytes;      // floats of a wave's tile, bytes of a wave's LDS (a multiple of 16)
 };
 
 struct Item {
     double lp;
-    float m, l2s, H, pad;  // m = -inf: an empty segment
+    float m, l2s, H;  // m = -inf: an empty segment
+    int act;
 };
 
 struct TypesIO {
@@ -840,22 +864,37 @@ __device__ __forceinline__ void load_tile(const T *z, int64_t ld, int a, int n, 
     const int total = n * a;
     if (ld == a) {  // one run of columns: vectors behind the first aligned one, which zs was placed for
         if (lane < head && lane < total) zs[lane] = to_f32(z[lane]);
-        const int full = max(total - head, 0) / N;
-        for (int v = lane; v < full; v += 64) {
-            float x[N];
-            unpack(reinterpret_cast<const uint4 *>(z + head)[v], x);
-            float4 *d = reinterpret_cast<float4 *>(zs + head + v * N);
+        const int full = max(total - head, 0) / N, last = head + full * N + lane;
+        const uint4 *body = reinterpret_cast<const uint4 *>(z + head);
+        float tail = 0.f;
+        if (last < total) tail = to_f32(z[last]);
+        for (int v = lane; v < full; v += 256) {
+            uint4 raw[4];  // four loads in flight; beyond the end the last vector again
 #pragma unroll
-            for (int i = 0; i < N / 4; ++i) d[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+            for (int j = 0; j < 4; ++j) raw[j] = body[min(v + 64 * j, full - 1)];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (v + 64 * j >= full) break;
+                float x[N];
+                unpack(raw[j], x);
+                float4 *d = reinterpret_cast<float4 *>(zs + head + (v + 64 * j) * N);
+#pragma unroll
+                for (int i = 0; i < N / 4; ++i) d[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+            }
         }
-        const int e = head + full * N + lane;
-        if (e < total) zs[e] = to_f32(z[e]);
+        if (last < total) zs[last] = tail;
         return;
     }
-#pragma unroll 4
-    for (int e = lane; e < total; e += 64) {
-        const int r = (int)__umulhi((uint32_t)e, magic);
-        zs[e] = to_f32(z[r * ld + (e - r * a)]);
+    for (int e = lane; e < total; e += 256) {
+        float x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int i = min(e + 64 * j, total - 1), r = (int)__umulhi((uint32_t)i, magic);
+            x[j] = to_f32(z[r * ld + (i - r * a)]);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (e + 64 * j < total) zs[e + 64 * j] = x[j];
     }
 }
 
@@ -915,18 +954,35 @@ __global__ __launch_bounds__(kThreads) void k_types(Rows q, TypesShape sh, Types
         const T *z = static_cast<const T *>(q.z) + r0 * q.ld;
         const int mis = (int)(reinterpret_cast<uintptr_t>(z) / sizeof(T)) & (N - 1), head = mis ? N - mis : 0;
         float *zs = tile + ((4 - head) & 3);
+        // everything else of the rows is loaded beside their logits
+        for (int p = lane; p < items; p += 64) item[p].act = q.act[r0 * ns + p];
+        const bool own = lane < n;
+        const int64_t r = r0 + lane;
+        float w = 1.f, old = 0.f, ref = 0.f, adv = 0.f;
+        if (own && MODE == kTypesDiff) {
+            if (q.weight) w = q.weight[r];
+            if (io.logp_ref) ref = io.logp_ref[r];
+        }
+        if (own && MODE == kTypesLoss) {
+            w = io.loss.weight ? io.loss.weight[r] : io.loss.inv_m;
+            old = io.loss.logp_old[r];
+            adv = io.loss.adv[r];
+            if (io.loss.logp_ref) ref = io.loss.logp_ref[r];
+        }
         load_tile<T>(z, q.ld, a, n, sh.magic, head, zs, lane);
         wave_sync();
         if (!kGradOnly) {
             for (int p = g0; p < items; p += gn) {
-                const int r = p / ns, s = p - r * ns, i1 = off[s + 1];
-                const float *x = zs + r * a;
+                const int ri = p * sh.seg_magic >> 16, s = p - ri * ns, i0 = off[s], i1 = off[s + 1];
+                const float *x = zs + ri * a;
                 float m = -INFINITY;
-                for (int i = off[s] + gl; i < i1; i += L) m = max_nan(m, x[i]);
+#pragma unroll 4
+                for (int i = i0 + gl; i < i1; i += L) m = max_nan(m, x[i]);
                 m = group_reduce(m, L, -INFINITY, [](float b, float c) { return max_nan(b, c); });
                 const float ms = shift_of(m);
                 Sums sum{m, 0.f, 0.f};
-                for (int i = off[s] + gl; i < i1; i += L) {
+#pragma unroll 4
+                for (int i = i0 + gl; i < i1; i += L) {
                     const float y = fmaxf((x[i] - ms) * kLog2e, kYMin), e = exp2_hw(y);
                     sum.s += e;
                     sum.u = fmaf(e, y, sum.u);
@@ -936,43 +992,41 @@ __global__ __launch_bounds__(kThreads) void k_types(Rows q, TypesShape sh, Types
                 sum.u = group_reduce(sum.u, L, 0.f, add);
                 if (!(m < INFINITY)) sum.s = sum.u = __builtin_nanf("");
                 if (gl != 0) continue;
-                const int64_t e = (r0 + r) * ns + s;
-                const float zact = x[min(max(q.act[e], off[s]), i1 - 1)];
-                Item it{};
-                it.m = sum.s == 0.f ? -INFINITY : m;
-                it.l2s = __builtin_amdgcn_logf(sum.s);
-                it.lp = log_prob(sum, zact);
-                if (MODE == kTypesLoss) it.H = (float)entropy_of(sum);
-                if (MODE == kTypesDiff) io.norm[e] = make_float2(it.m, it.l2s);
-                if (MODE == kTypesLogp && io.entropy) io.entropy[e] = (float)entropy_of(sum);
+                const float zact = x[min(max(item[p].act, i0), i1 - 1)];
+                const LogSum l = log_sum_f32(sum);
+                const int64_t e = r0 * ns + p;
+                item[p].m = sum.s == 0.f ? -INFINITY : m;
+                item[p].l2s = l.l2s;
+                if (MODE == kTypesDiff) {  // long sums of small differences follow: 64 bits
+                    item[p].lp = log_prob(sum, zact);
+                    io.norm[e] = make_float2(sum.s == 0.f ? -INFINITY : m, l.l2s);
+                    continue;
+                }
+                const float H = entropy_f32(sum, l);
+                item[p].lp = (double)log_prob_f32(sum, l, zact);
+                item[p].H = H;
+                if (MODE == kTypesLogp && io.entropy) io.entropy[e] = H;
                 if (MODE == kTypesLogp && io.lse) {
                     io.lse[2 * e] = m;
-                    io.lse[2 * e + 1] = sum.s == 0.f ? 0.f : (float)log_sum(sum);
+                    io.lse[2 * e + 1] = sum.s == 0.f ? 0.f : l.ls;
                 }
-                item[p] = it;
             }
             wave_sync();
         }
-        if (lane < n) {
-            const int64_t r = r0 + lane;
+        if (own) {
             double lp = 0.0, H = 0.0;
             if (!kGradOnly)
                 for (int s = 0; s < ns; ++s) {
                     lp += item[lane * ns + s].lp;
-                    H += (double)item[lane * ns + s].H;
+                    if (MODE == kTypesLoss) H += (double)item[lane * ns + s].H;
                 }
             float2 g = make_float2(0.f, 0.f);
             if (MODE == kTypesLogp) io.logp[r] = (float)lp;
-            if (MODE == kTypesDiff) {
-                const float w = q.weight ? q.weight[r] : 1.f;
-                io.diff[r] = w == 0.f ? 0.0 : (double)w * (lp - (io.logp_ref ? (double)io.logp_ref[r] : 0.0));
-            }
+            if (MODE == kTypesDiff) io.diff[r] = w == 0.f ? 0.0 : (double)w * (lp - (double)ref);
             if (MODE == kTypesLoss) {
-                const float w = io.loss.weight ? io.loss.weight[r] : io.loss.inv_m;
                 if (w != 0.f) {
                     float surrogate, kl;
-                    loss_grad(io.loss, w, io.loss.logp_old[r], io.loss.logp_ref ? io.loss.logp_ref[r] : 0.f, io.loss.adv[r], (float)lp,
-                              g.x, g.y, surrogate, kl);
+                    loss_grad(io.loss, w, old, ref, adv, (float)lp, g.x, g.y, surrogate, kl);
                     acc[0] -= (double)w * (double)surrogate;
                     acc[1] += (double)w * (double)kl;
                     acc[2] += (double)w * H;
@@ -986,10 +1040,10 @@ __global__ __launch_bounds__(kThreads) void k_types(Rows q, TypesShape sh, Types
         wave_sync();
         if (MODE == kTypesLogp || MODE == kTypesDiff || !io.dz) continue;
         for (int p = g0; p < items; p += gn) {
-            const int r = p / ns, s = p - r * ns, i1 = off[s + 1];
-            const int64_t e = (r0 + r) * ns + s;
-            float *x = zs + r * a;
-            const float2 g = row[r];
+            const int ri = p * sh.seg_magic >> 16, s = p - ri * ns, i0 = off[s], i1 = off[s + 1];
+            const int64_t e = r0 * ns + p;
+            float *x = zs + ri * a;
+            const float2 g = row[ri];
             float m, l2s, H = 0.f;
             if (MODE == kTypesLoss) {
                 m = item[p].m, l2s = item[p].l2s, H = item[p].H;
@@ -1002,11 +1056,17 @@ __global__ __launch_bounds__(kThreads) void k_types(Rows q, TypesShape sh, Types
             }
             const RowCoef k = coef_of(m, m == -INFINITY ? 0.f : 1.f, l2s, H, g.x, g.y);
             if (k.zero != 0.f) {
-                for (int i = off[s] + gl; i < i1; i += L) x[i] = 0.f;
+                for (int i = i0 + gl; i < i1; i += L) x[i] = 0.f;
                 continue;
             }
-            const int act = min(max(q.act[e], off[s]), i1 - 1);
-            for (int i = off[s] + gl; i < i1; i += L) x[i] = grad_any(k, x[i]) + (i == act ? k.g : 0.f);
+            const int act = min(max(item[p].act, i0), i1 - 1);
+            if (k.e != 0.f) {
+#pragma unroll 4
+                for (int i = i0 + gl; i < i1; i += L) x[i] = grad_of<true>(k, x[i]) + (i == act ? k.g : 0.f);
+            } else {
+#pragma unroll 4
+                for (int i = i0 + gl; i < i1; i += L) x[i] = grad_of<false>(k, x[i]) + (i == act ? k.g : 0.f);
+            }
         }
         wave_sync();
         store_tile<T>(static_cast<T *>(io.dz) + r0 * io.ld_d, io.ld_d, a, n, sh.magic, head, zs, lane);
@@ -1126,6 +1186,7 @@ TypesShape types_shape(const harl_policy_head *h, int32_t M) {
     while (lanes < 64 && lanes < longest && lanes * 2 * s.rows * h->n_seg <= 64) lanes *= 2;
     s.lanes = lanes;
     s.magic = (uint32_t)((((uint64_t)1 << 32) + h->a - 1) / h->a);
+    s.seg_magic = (65536 + h->n_seg - 1) / h->n_seg;
     s.tile = (int)round_up((int64_t)s.rows * h->a + 4, 4);
     s.bytes = s.tile * 4 + s.rows * h->n_seg * (int)sizeof(Item) + (int)round_up(s.rows * 8, 16);
     return s;

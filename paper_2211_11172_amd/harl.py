@@ -197,10 +197,22 @@ def _ptr(x):
     return x.data_ptr()
 
 
+_raw_stream = None  # torch's current stream of a device as an integer
+
+
 def _stream(s):
+    """``None`` is torch's current stream on the current device.  Its raw handle is read without building a
+    Stream object, which took 2.6 of the 4.5 us that a call spent here."""
+    global _raw_stream
     if s is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        if _raw_stream is None:
+            import torch
+            raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+            if raw is None:
+                _raw_stream = lambda: torch.cuda.current_stream().cuda_stream  # noqa: E731
+            else:
+                _raw_stream = lambda: raw(torch.cuda.current_device())  # noqa: E731
+        return _raw_stream()
     if isinstance(s, int):
         return s
     return s.cuda_stream
