@@ -73,35 +73,6 @@ __device__ __forceinline__ void loss_row(const LossArgs &a, int64_t r, float w, 
     term[2] = (double)w * H;
 }
 
-// Sums of N terms per row over n rows by one workgroup: thread-strided in row order, then a tree.
-template <int N>
-__device__ __forceinline__ void sum_terms(const double *__restrict__ terms, int64_t n, double (&out)[N]) {
-    __shared__ double part[N][kThreads];
-    double s[N] = {};
-    for (int64_t r = threadIdx.x; r < n; r += kThreads)
-        for (int c = 0; c < N; ++c) s[c] += terms[r * N + c];
-    for (int c = 0; c < N; ++c) part[c][threadIdx.x] = s[c];
-    __syncthreads();
-    for (int h = kThreads / 2; h > 0; h >>= 1) {
-        if ((int)threadIdx.x < h)
-            for (int c = 0; c < N; ++c) part[c][threadIdx.x] += part[c][threadIdx.x + h];
-        __syncthreads();
-    }
-    for (int c = 0; c < N; ++c) out[c] = part[c][0];
-}
-
-__device__ __forceinline__ void write_loss(const double (&s)[3], float w_kl, float w_entropy, float *loss) {
-    loss[0] = (float)(s[0] + (w_kl != 0.f ? (double)w_kl * s[1] : 0.0) - (w_entropy != 0.f ? (double)w_entropy * s[2] : 0.0));
-    for (int c = 0; c < 3; ++c) loss[1 + c] = (float)s[c];
-}
-
-__global__ __launch_bounds__(kThreads) void k_loss_sum(const double *__restrict__ terms, int64_t n, float w_kl,
-                                                       float w_entropy, float *__restrict__ loss) {
-    double s[3];
-    sum_terms<3>(terms, n, s);
-    if (threadIdx.x == 0) write_loss(s, w_kl, w_entropy, loss);
-}
-
 // ------------------------------------------------------------------------------------------------
 // Heads of one segment.  A row is moved as 16-byte vectors behind its first aligned column; the columns
 // before it and behind the last whole vector (at most 2 (16 / element - 1)) are an element a thread.
@@ -222,6 +193,20 @@ __device__ __forceinline__ Sums lanes_join(Sums q) {
     rescale(q, m, shift_of(m));
     const auto add = [](float a, float b) { return a + b; };
     return Sums{m, lanes_reduce<W>(q.s, 0.f, add), lanes_reduce<W>(q.u, 0.f, add)};
+}
+
+// Sum of 64 bits over a wave, in lane order by pairs; the result in every lane.
+__device__ __forceinline__ double wave_sum(double x) {
+    const auto move = [](double v, auto f) {
+        return __hiloint2double(__float_as_int(f(__int_as_float(__double2hiint(v)))), __float_as_int(f(__int_as_float(__double2loint(v)))));
+    };
+    x += move(x, [](float v) { return dpp<0x111, 0xf>(v, 0.f); });
+    x += move(x, [](float v) { return dpp<0x112, 0xf>(v, 0.f); });
+    x += move(x, [](float v) { return dpp<0x114, 0xf>(v, 0.f); });
+    x += move(x, [](float v) { return dpp<0x118, 0xf>(v, 0.f); });
+    x += move(x, [](float v) { return dpp<0x142, 0xa>(v, 0.f); });
+    x += move(x, [](float v) { return dpp<0x143, 0xc>(v, 0.f); });
+    return move(x, [](float v) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63)); });
 }
 
 // The sums of a row from those of its TPR threads, in every thread.  `red` has 2 halves of TPR / 64
@@ -577,6 +562,40 @@ __global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void k_loss(Rows q
     }
 }
 
+// Sums of N terms over n entries by one workgroup: thread-strided in order, then over lanes and waves.
+template <int N>
+__device__ __forceinline__ void sum_terms(const double *__restrict__ terms, int64_t n, double (&out)[N]) {
+    __shared__ double part[N][kThreads / 64];
+    double s[N] = {};
+#pragma unroll 4
+    for (int64_t r = threadIdx.x; r < n; r += kThreads)
+#pragma unroll
+        for (int c = 0; c < N; ++c) s[c] += terms[r * N + c];
+#pragma unroll
+    for (int c = 0; c < N; ++c) {
+        s[c] = wave_sum(s[c]);
+        if (threadIdx.x % 64 == 0) part[c][threadIdx.x / 64] = s[c];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int c = 0; c < N; ++c) {
+        out[c] = part[c][0];
+        for (int w = 1; w < kThreads / 64; ++w) out[c] += part[c][w];
+    }
+}
+
+__device__ __forceinline__ void write_loss(const double (&s)[3], float w_kl, float w_entropy, float *loss) {
+    loss[0] = (float)(s[0] + (w_kl != 0.f ? (double)w_kl * s[1] : 0.0) - (w_entropy != 0.f ? (double)w_entropy * s[2] : 0.0));
+    for (int c = 0; c < 3; ++c) loss[1 + c] = (float)s[c];
+}
+
+__global__ __launch_bounds__(kThreads) void k_loss_sum(const double *__restrict__ terms, int64_t n, float w_kl,
+                                                       float w_entropy, float *__restrict__ loss) {
+    double s[3];
+    sum_terms<3>(terms, n, s);
+    if (threadIdx.x == 0) write_loss(s, w_kl, w_entropy, loss);
+}
+
 // ---- preference loss ----
 // A row for the gradient pass of one segment: m, log2 s and the gradient of its log-probability.
 struct RowFin {
@@ -621,8 +640,7 @@ __global__ __launch_bounds__(kThreads) void k_pairs(PairArgs a, const Stat *__re
             s[r >= mid ? 1 : 0] += d;
         }
         for (int side = 0; side < 2; ++side) {
-            double v = s[side];
-            for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+            const double v = wave_sum(s[side]);
             if (threadIdx.x % 64 == 0) part[half][side][threadIdx.x / 64] = v;
         }
         __syncthreads();
@@ -703,7 +721,7 @@ __device__ __forceinline__ Sums join_wave(const Stat *__restrict__ st, int chunk
 
 // Few rows' loss terms by one workgroup: a thread a row where rows have few chunks, else a wave a row.
 __device__ void loss_of_rows(const GradSrc &a, int M) {
-    __shared__ double part[3][kThreads];
+    __shared__ double part[3][kThreads / 64];
     double acc[3] = {0.0, 0.0, 0.0};
     const bool wave = a.stat_chunks > 16;
     const int step = wave ? kThreads / 64 : kThreads;
@@ -723,15 +741,15 @@ __device__ void loss_of_rows(const GradSrc &a, int M) {
         for (int c = 0; c < 3; ++c) acc[c] += term[c];
         if (a.logp) a.logp[r] = (float)lp;
     }
-    for (int c = 0; c < 3; ++c) part[c][threadIdx.x] = acc[c];
-    __syncthreads();
-    for (int h = kThreads / 2; h > 0; h >>= 1) {
-        if ((int)threadIdx.x < h)
-            for (int c = 0; c < 3; ++c) part[c][threadIdx.x] += part[c][threadIdx.x + h];
-        __syncthreads();
+    for (int c = 0; c < 3; ++c) {
+        const double v = wave_sum(acc[c]);
+        if (threadIdx.x % 64 == 0) part[c][threadIdx.x / 64] = v;
     }
+    __syncthreads();
     if (threadIdx.x == 0 && a.loss_out) {
-        const double s[3] = {part[0][0], part[1][0], part[2][0]};
+        double s[3] = {};
+        for (int c = 0; c < 3; ++c)
+            for (int i = 0; i < kThreads / 64; ++i) s[c] += part[c][i];
         write_loss(s, a.loss.w_kl, a.loss.w_entropy, a.loss_out);
     }
 }
@@ -815,11 +833,18 @@ enum TypesMode : int { kTypesLogp, kTypesDiff, kTypesLoss, kTypesGradLse, kTypes
 
 constexpr int kTypesItems = 256;  // (row, segment) items of a wave at most
 constexpr int kTypesTile = 2048;  // columns of a wave's rows at most, or one row
+constexpr int kTypesTable = 2 * HARL_SELECT_MAX_SEGMENTS + 4;  // ints of a wave's copy of the segments' offsets and order
+
+// Segments fall into two classes by length, so that a long segment's lanes do not idle at short ones.
+struct TypesClass {
+    int n, lanes, magic;  // segments of the class, lanes of an item, ceil(2^16 / n): p / n = p magic >> 16
+};
 
 struct TypesShape {
-    int rows, lanes;      // rows of a wave, lanes of an item
+    int rows;             // rows of a wave
+    TypesClass cls[2];    // long and short segments
+    uint8_t order[HARL_SELECT_MAX_SEGMENTS];  // segments, the long ones first
     uint32_t magic;       // ceil(2^32 / a): e / a = umulhi(e, magic) for the tile's e
-    int seg_magic;        // ceil(2^16 / n_seg): p / n_seg = p seg_magic >> 16 for a wave's items
     int tile, bytes;      // floats of a wave's tile, bytes of a wave's LDS (a multiple of 16)
 };
 
@@ -850,12 +875,43 @@ __device__ __forceinline__ void wave_sync() {  // LDS serves a wave's accesses i
     __builtin_amdgcn_wave_barrier();
 }
 
-// max / sum over groups of `lanes` consecutive lanes, in every lane of the group
+// max / sum over groups of `lanes` consecutive lanes (a power of two, the same for the wave), in every
+// lane of the group: within 16 lanes by data-parallel moves, which cost a tenth of a shuffle
 template <typename Op>
 __device__ __forceinline__ float group_reduce(float x, int lanes, float none, Op op) {
     if (lanes == 64) return lanes_reduce<64>(x, none, op);
-    for (int o = lanes / 2; o > 0; o >>= 1) x = op(x, __shfl_xor(x, o));
+    if (lanes > 1) x = op(x, dpp<0xb1, 0xf>(x, none));   // quad_perm 1 0 3 2
+    if (lanes > 2) x = op(x, dpp<0x4e, 0xf>(x, none));   // quad_perm 2 3 0 1
+    if (lanes > 4) x = op(x, dpp<0x141, 0xf>(x, none));  // row_half_mirror: the other four of eight
+    if (lanes > 8) x = op(x, dpp<0x140, 0xf>(x, none));  // row_mirror: the other eight of sixteen
+    if (lanes > 16) x = op(x, __shfl_xor(x, 16));
     return x;
+}
+
+// A long segment [i0, i1) of row x by the wave, four columns a lane from 16-byte aligned places of the
+// tile: f(i, i + 4, values) with -inf in the places of other segments' columns.
+template <typename F>
+__device__ __forceinline__ void for_vectors(const float *x, const float *tile, int i0, int i1, int lane, F f) {
+    const int at = (int)(x - tile);
+    for (int i = ((at + i0) & ~3) - at + 4 * lane; i < i1; i += 256) {
+        const float4 q = *reinterpret_cast<const float4 *>(x + i);
+        float v[4] = {q.x, q.y, q.z, q.w};
+        if (i < i0 || i + 4 > i1) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (i + j < i0 || i + j >= i1) v[j] = -INFINITY;
+        }
+        f(i, i + 4, v);
+    }
+}
+__device__ __forceinline__ void put_vector(float *x, int from, int to, int i0, int i1, const float (&f)[4]) {
+    if (from >= i0 && to <= i1) {
+        *reinterpret_cast<float4 *>(x + from) = make_float4(f[0], f[1], f[2], f[3]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (from + j >= i0 && from + j < i1) x[from + j] = f[j];
+    }
 }
 
 template <typename T>
@@ -932,22 +988,20 @@ __global__ __launch_bounds__(kThreads) void k_types(Rows q, TypesShape sh, Types
     constexpr int N = kVec<T>;
     constexpr bool kGradOnly = MODE == kTypesGradLse || MODE == kTypesGradPairs;
     extern __shared__ __attribute__((aligned(16))) char smem[];
-    __shared__ int off[HARL_SELECT_MAX_SEGMENTS + 1];
     if (MODE == kTypesGradPairs && io.loss_out && blockIdx.x == gridDim.x - 1) {
         pairs_sum(io.pair_terms, io.n_pairs, io.loss_out);
         return;
     }
     const unsigned groups = gridDim.x - (MODE == kTypesGradPairs && io.loss_out ? 1 : 0);
-    if (threadIdx.x <= (unsigned)q.n_seg) off[threadIdx.x] = q.off[threadIdx.x];
-    __syncthreads();
     const int wv = threadIdx.x / 64, lane = threadIdx.x % 64, ns = q.n_seg, a = q.a;
     const int items_max = sh.rows * ns;
     char *mine = smem + wv * sh.bytes;
     float *tile = reinterpret_cast<float *>(mine);
     Item *item = reinterpret_cast<Item *>(mine + (size_t)sh.tile * 4);
     float2 *row = reinterpret_cast<float2 *>(item + items_max);  // a row's gradients of log-probability and entropy
+    int *off = reinterpret_cast<int *>(mine + sh.bytes) - kTypesTable, *order = off + HARL_SELECT_MAX_SEGMENTS + 1;
+    const int my_off = lane <= ns ? q.off[lane] : 0, my_order = lane < ns ? sh.order[lane] : 0;
     const int lo = q.seq_ptr ? clamp_row(q.seq_ptr[0], q.M) : 0, hi = q.seq_ptr ? clamp_row(q.seq_ptr[q.n_seq], q.M) : q.M;
-    const int L = sh.lanes, gl = lane % L, g0 = lane / L, gn = 64 / L;
     double acc[3] = {0.0, 0.0, 0.0};
     for (int64_t r0 = lo + ((int64_t)blockIdx.x * 4 + wv) * sh.rows; r0 < hi; r0 += (int64_t)groups * 4 * sh.rows) {
         const int n = (int)min((int64_t)sh.rows, hi - r0), items = n * ns;
@@ -955,7 +1009,7 @@ __global__ __launch_bounds__(kThreads) void k_types(Rows q, TypesShape sh, Types
         const int mis = (int)(reinterpret_cast<uintptr_t>(z) / sizeof(T)) & (N - 1), head = mis ? N - mis : 0;
         float *zs = tile + ((4 - head) & 3);
         // everything else of the rows is loaded beside their logits
-        for (int p = lane; p < items; p += 64) item[p].act = q.act[r0 * ns + p];
+        const int act0 = lane < items ? q.act[r0 * ns + lane] : 0;
         const bool own = lane < n;
         const int64_t r = r0 + lane;
         float w = 1.f, old = 0.f, ref = 0.f, adv = 0.f;
@@ -970,22 +1024,43 @@ __global__ __launch_bounds__(kThreads) void k_types(Rows q, TypesShape sh, Types
             if (io.loss.logp_ref) ref = io.loss.logp_ref[r];
         }
         load_tile<T>(z, q.ld, a, n, sh.magic, head, zs, lane);
+        if (lane < items) item[lane].act = act0;
+        for (int p = lane + 64; p < items; p += 64) item[p].act = q.act[r0 * ns + p];
+        if (lane <= ns) off[lane] = my_off;
+        if (lane < ns) order[lane] = my_order;
         wave_sync();
         if (!kGradOnly) {
-            for (int p = g0; p < items; p += gn) {
-                const int ri = p * sh.seg_magic >> 16, s = p - ri * ns, i0 = off[s], i1 = off[s + 1];
+#pragma unroll 1
+          for (int cl = 0; cl < 2; ++cl) {
+            const TypesClass tc = sh.cls[cl];
+            const int L = tc.lanes, gl = lane & (L - 1), gn = 64 / L;
+            for (int w0 = lane / L; w0 < n * tc.n; w0 += gn) {
+                const int ri = w0 * tc.magic >> 16, s = order[(cl ? sh.cls[0].n : 0) + w0 - ri * tc.n], p = ri * ns + s;
+                const int i0 = off[s], i1 = off[s + 1];
                 const float *x = zs + ri * a;
                 float m = -INFINITY;
+                if (L == 64) {
+                    for_vectors(x, tile, i0, i1, lane, [&](int, int, float (&f)[4]) { m = max_nan(max_nan(m, f[0]), max_nan(f[1], max_nan(f[2], f[3]))); });
+                } else {
 #pragma unroll 4
-                for (int i = i0 + gl; i < i1; i += L) m = max_nan(m, x[i]);
+                    for (int i = i0 + gl; i < i1; i += L) m = max_nan(m, x[i]);
+                }
                 m = group_reduce(m, L, -INFINITY, [](float b, float c) { return max_nan(b, c); });
                 const float ms = shift_of(m);
                 Sums sum{m, 0.f, 0.f};
-#pragma unroll 4
-                for (int i = i0 + gl; i < i1; i += L) {
-                    const float y = fmaxf((x[i] - ms) * kLog2e, kYMin), e = exp2_hw(y);
+                const auto add_one = [&](float z1) {
+                    const float y = fmaxf((z1 - ms) * kLog2e, kYMin), e = exp2_hw(y);
                     sum.s += e;
                     sum.u = fmaf(e, y, sum.u);
+                };
+                if (L == 64) {
+                    for_vectors(x, tile, i0, i1, lane, [&](int, int, float (&f)[4]) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) add_one(f[j]);
+                    });
+                } else {
+#pragma unroll 4
+                    for (int i = i0 + gl; i < i1; i += L) add_one(x[i]);
                 }
                 const auto add = [](float b, float c) { return b + c; };
                 sum.s = group_reduce(sum.s, L, 0.f, add);
@@ -1011,6 +1086,7 @@ __global__ __launch_bounds__(kThreads) void k_types(Rows q, TypesShape sh, Types
                     io.lse[2 * e + 1] = sum.s == 0.f ? 0.f : l.ls;
                 }
             }
+          }
             wave_sync();
         }
         if (own) {
@@ -1039,8 +1115,13 @@ __global__ __launch_bounds__(kThreads) void k_types(Rows q, TypesShape sh, Types
         }
         wave_sync();
         if (MODE == kTypesLogp || MODE == kTypesDiff || !io.dz) continue;
-        for (int p = g0; p < items; p += gn) {
-            const int ri = p * sh.seg_magic >> 16, s = p - ri * ns, i0 = off[s], i1 = off[s + 1];
+#pragma unroll 1
+        for (int cl = 0; cl < 2; ++cl) {
+          const TypesClass tc = sh.cls[cl];
+          const int L = tc.lanes, gl = lane & (L - 1), gn = 64 / L;
+          for (int w0 = lane / L; w0 < n * tc.n; w0 += gn) {
+            const int ri = w0 * tc.magic >> 16, s = order[(cl ? sh.cls[0].n : 0) + w0 - ri * tc.n], p = ri * ns + s;
+            const int i0 = off[s], i1 = off[s + 1];
             const int64_t e = r0 * ns + p;
             float *x = zs + ri * a;
             const float2 g = row[ri];
@@ -1060,13 +1141,26 @@ __global__ __launch_bounds__(kThreads) void k_types(Rows q, TypesShape sh, Types
                 continue;
             }
             const int act = min(max(item[p].act, i0), i1 - 1);
-            if (k.e != 0.f) {
+            if (L == 64) {
+                for_vectors(x, tile, i0, i1, lane, [&](int from, int to, float (&f)[4]) {
+                    if (k.e != 0.f) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) f[j] = grad_of<true>(k, f[j]);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) f[j] = grad_of<false>(k, f[j]);
+                    }
+                    put_vector(x, from, to, i0, i1, f);
+                });
+            } else if (k.e != 0.f) {
 #pragma unroll 4
-                for (int i = i0 + gl; i < i1; i += L) x[i] = grad_of<true>(k, x[i]) + (i == act ? k.g : 0.f);
+                for (int i = i0 + gl; i < i1; i += L) x[i] = grad_of<true>(k, x[i]);
             } else {
 #pragma unroll 4
-                for (int i = i0 + gl; i < i1; i += L) x[i] = grad_of<false>(k, x[i]) + (i == act ? k.g : 0.f);
+                for (int i = i0 + gl; i < i1; i += L) x[i] = grad_of<false>(k, x[i]);
             }
+            if (gl == 0) x[act] += k.g;  // behind the group's writes: LDS serves a wave in order
+          }
         }
         wave_sync();
         store_tile<T>(static_cast<T *>(io.dz) + r0 * io.ld_d, io.ld_d, a, n, sh.magic, head, zs, lane);
@@ -1076,8 +1170,7 @@ __global__ __launch_bounds__(kThreads) void k_types(Rows q, TypesShape sh, Types
         __shared__ double part[4][3];
 #pragma unroll
         for (int c = 0; c < 3; ++c) {
-            double v = acc[c];
-            for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+            const double v = wave_sum(acc[c]);
             if (lane == 0) part[wv][c] = v;
         }
         __syncthreads();
@@ -1180,15 +1273,30 @@ TypesShape types_shape(const harl_policy_head *h, int32_t M) {
     // enough waves to fill the machine (8 a SIMD), rows enough to keep a wave's loads wide
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>({64, kTypesItems / h->n_seg, kTypesTile / h->a}));
     s.rows = (int)std::max<int64_t>(1, std::min<int64_t>(most, ceil_div(M, 8192)));
-    // lanes for about 16 columns each of the longest segment, more where a wave has too few items for its lanes
-    int lanes = 1;
-    while (lanes < 64 && lanes * 16 < longest) lanes *= 2;
-    while (lanes < 64 && lanes < longest && lanes * 2 * s.rows * h->n_seg <= 64) lanes *= 2;
-    s.lanes = lanes;
+    // long segments: more than a quarter of the longest, where that fills a wave by itself; two classes take
+    // 3 us longer than one where it does not
+    const int split = longest > 256 ? longest : 0;
+    int at = 0;
+    for (int c = 0; c < 2; ++c) {
+        int top = 0;
+        for (int i = 0; i < h->n_seg; ++i) {
+            const int len = h->seg_offsets[i + 1] - h->seg_offsets[i];
+            if ((len * 4 > split) == (c == 1)) continue;
+            s.order[at++] = (uint8_t)i;
+            ++s.cls[c].n;
+            top = std::max(top, len);
+        }
+        // lanes for about 16 columns each, more where a wave has too few items for its lanes
+        const int items = s.rows * s.cls[c].n;
+        int lanes = 1;
+        while (lanes < 64 && lanes * 16 < top) lanes *= 2;
+        while (lanes < 64 && lanes < top && lanes * 2 * items <= 64) lanes *= 2;
+        s.cls[c].lanes = lanes;
+        s.cls[c].magic = s.cls[c].n ? (65536 + s.cls[c].n - 1) / s.cls[c].n : 0;
+    }
     s.magic = (uint32_t)((((uint64_t)1 << 32) + h->a - 1) / h->a);
-    s.seg_magic = (65536 + h->n_seg - 1) / h->n_seg;
     s.tile = (int)round_up((int64_t)s.rows * h->a + 4, 4);
-    s.bytes = s.tile * 4 + s.rows * h->n_seg * (int)sizeof(Item) + (int)round_up(s.rows * 8, 16);
+    s.bytes = s.tile * 4 + s.rows * h->n_seg * (int)sizeof(Item) + (int)round_up(s.rows * 8, 16) + kTypesTable * 4;
     return s;
 }
 
