@@ -12,6 +12,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "internal.hpp"
 
@@ -241,7 +242,7 @@ struct LogSum {
     float l2s, ls, mean_y;
 };
 __device__ __forceinline__ LogSum log_sum_f32(const Sums &q) {
-    const float l2s = __builtin_amdgcn_logf(q.s), mean_y = q.u / q.s;
+    const float l2s = __builtin_amdgcn_logf(q.s), mean_y = q.u * __builtin_amdgcn_rcpf(q.s);
     return LogSum{l2s, fmaf(l2s, kLn2, (float)(kLog2eRest * kLn2d * kLn2d) * mean_y), mean_y};
 }
 __device__ __forceinline__ float log_prob_f32(const Sums &q, const LogSum &l, float zact) { return q.s == 0.f ? 0.f : (zact - q.m) - l.ls; }
@@ -875,21 +876,21 @@ __device__ __forceinline__ void wave_sync() {  // LDS serves a wave's accesses i
     __builtin_amdgcn_wave_barrier();
 }
 
-// max / sum over groups of `lanes` consecutive lanes (a power of two, the same for the wave), in every
-// lane of the group: within 16 lanes by data-parallel moves, which cost a tenth of a shuffle
-template <typename Op>
-__device__ __forceinline__ float group_reduce(float x, int lanes, float none, Op op) {
-    if (lanes == 64) return lanes_reduce<64>(x, none, op);
-    if (lanes > 1) x = op(x, dpp<0xb1, 0xf>(x, none));   // quad_perm 1 0 3 2
-    if (lanes > 2) x = op(x, dpp<0x4e, 0xf>(x, none));   // quad_perm 2 3 0 1
-    if (lanes > 4) x = op(x, dpp<0x141, 0xf>(x, none));  // row_half_mirror: the other four of eight
-    if (lanes > 8) x = op(x, dpp<0x140, 0xf>(x, none));  // row_mirror: the other eight of sixteen
-    if (lanes > 16) x = op(x, __shfl_xor(x, 16));
+// max / sum over groups of L consecutive lanes, in every lane of the group: within 16 lanes by data-parallel
+// moves, which cost a tenth of a shuffle
+template <int L, typename Op>
+__device__ __forceinline__ float group_reduce(float x, float none, Op op) {
+    if constexpr (L == 64) return lanes_reduce<64>(x, none, op);
+    if constexpr (L > 1) x = op(x, dpp<0xb1, 0xf>(x, none));   // quad_perm 1 0 3 2
+    if constexpr (L > 2) x = op(x, dpp<0x4e, 0xf>(x, none));   // quad_perm 2 3 0 1
+    if constexpr (L > 4) x = op(x, dpp<0x141, 0xf>(x, none));  // row_half_mirror: the other four of eight
+    if constexpr (L > 8) x = op(x, dpp<0x140, 0xf>(x, none));  // row_mirror: the other eight of sixteen
+    if constexpr (L > 16) x = op(x, __shfl_xor(x, 16));
     return x;
 }
 
 // A long segment [i0, i1) of row x by the wave, four columns a lane from 16-byte aligned places of the
-// tile: f(i, i + 4, values) with -inf in the places of other segments' columns.
+// tile: f(i, values) with -inf in the places of other segments' columns.
 template <typename F>
 __device__ __forceinline__ void for_vectors(const float *x, const float *tile, int i0, int i1, int lane, F f) {
     const int at = (int)(x - tile);
@@ -901,11 +902,11 @@ __device__ __forceinline__ void for_vectors(const float *x, const float *tile, i
             for (int j = 0; j < 4; ++j)
                 if (i + j < i0 || i + j >= i1) v[j] = -INFINITY;
         }
-        f(i, i + 4, v);
+        f(i, v);
     }
 }
-__device__ __forceinline__ void put_vector(float *x, int from, int to, int i0, int i1, const float (&f)[4]) {
-    if (from >= i0 && to <= i1) {
+__device__ __forceinline__ void put_vector(float *x, int from, int i0, int i1, const float (&f)[4]) {
+    if (from >= i0 && from + 4 <= i1) {
         *reinterpret_cast<float4 *>(x + from) = make_float4(f[0], f[1], f[2], f[3]);
     } else {
 #pragma unroll
@@ -983,6 +984,125 @@ __device__ __forceinline__ void store_tile(T *dz, int64_t ld, int a, int n, uint
     }
 }
 
+// A wave's rows in LDS.
+struct WaveTile {
+    float *tile, *zs;  // the tile, and its first row's first column
+    Item *item;
+    float2 *row;
+    const int *off;
+    int ns, a, lane;
+};
+
+// Sums of a class's items, L lanes each, and what follows from an item alone.  Lanes take four columns L apart
+// at a time; places behind a segment read its last column and add 0.
+template <int L, int MODE>
+__device__ __forceinline__ void types_sums(const WaveTile &w, const TypesIO &io, const TypesClass &tc, const int *segs, int64_t r0, int n) {
+    const int gl = w.lane % L;
+    for (int i = w.lane / L; i < n * tc.n; i += 64 / L) {
+        const int ri = i * tc.magic >> 16, s = segs[i - ri * tc.n], p = ri * w.ns + s, i0 = w.off[s], i1 = w.off[s + 1];
+        const float *x = w.zs + ri * w.a;
+        float m = -INFINITY;
+        if constexpr (L == 64) {
+            for_vectors(x, w.tile, i0, i1, w.lane, [&](int, const float (&f)[4]) { m = max_nan(max_nan(m, f[0]), max_nan(f[1], max_nan(f[2], f[3]))); });
+        } else {
+            for (int c = i0 + gl; c < i1; c += 4 * L)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) m = max_nan(m, x[min(c + j * L, i1 - 1)]);
+        }
+        m = group_reduce<L>(m, -INFINITY, [](float b, float c) { return max_nan(b, c); });
+        const float ms = shift_of(m);
+        Sums sum{m, 0.f, 0.f};
+        const auto add_one = [&](float z, bool in) {
+            const float y = in ? fmaxf((z - ms) * kLog2e, kYMin) : kYMin, e = exp2_hw(y);
+            sum.s += e;
+            sum.u = fmaf(e, y, sum.u);
+        };
+        if constexpr (L == 64) {
+            for_vectors(x, w.tile, i0, i1, w.lane, [&](int, const float (&f)[4]) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) add_one(f[j], true);
+            });
+        } else {
+            for (int c = i0 + gl; c < i1; c += 4 * L)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) add_one(x[min(c + j * L, i1 - 1)], c + j * L < i1);
+        }
+        const auto add = [](float b, float c) { return b + c; };
+        sum.s = group_reduce<L>(sum.s, 0.f, add);
+        sum.u = group_reduce<L>(sum.u, 0.f, add);
+        if (!(m < INFINITY)) sum.s = sum.u = __builtin_nanf("");
+        if (gl != 0) continue;
+        const float zact = x[min(max(w.item[p].act, i0), i1 - 1)];
+        const LogSum l = log_sum_f32(sum);
+        const int64_t e = r0 * w.ns + p;
+        w.item[p].m = sum.s == 0.f ? -INFINITY : m;
+        w.item[p].l2s = l.l2s;
+        if (MODE == kTypesDiff) {  // long sums of small differences follow: 64 bits
+            w.item[p].lp = log_prob(sum, zact);
+            io.norm[e] = make_float2(sum.s == 0.f ? -INFINITY : m, l.l2s);
+            continue;
+        }
+        const float H = entropy_f32(sum, l);
+        w.item[p].lp = (double)log_prob_f32(sum, l, zact);
+        w.item[p].H = H;
+        if (MODE == kTypesLogp && io.entropy) io.entropy[e] = H;
+        if (MODE == kTypesLogp && io.lse) {
+            io.lse[2 * e] = m;
+            io.lse[2 * e + 1] = sum.s == 0.f ? 0.f : l.ls;
+        }
+    }
+}
+
+// Gradients of a class's items in the place of their logits.
+template <int L, int MODE>
+__device__ __forceinline__ void types_grads(const WaveTile &w, const TypesIO &io, const TypesClass &tc, const int *segs, int64_t r0, int n) {
+    const int gl = w.lane % L;
+    for (int i = w.lane / L; i < n * tc.n; i += 64 / L) {
+        const int ri = i * tc.magic >> 16, s = segs[i - ri * tc.n], p = ri * w.ns + s, i0 = w.off[s], i1 = w.off[s + 1];
+        const int64_t e = r0 * w.ns + p;
+        float *x = w.zs + ri * w.a;
+        const float2 g = w.row[ri];
+        float m, l2s, H = 0.f;
+        if (MODE == kTypesLoss) {
+            m = w.item[p].m, l2s = w.item[p].l2s, H = w.item[p].H;
+        } else if (MODE == kTypesGradPairs) {
+            m = -INFINITY, l2s = 0.f;
+            if (g.x != 0.f) m = io.norm[e].x, l2s = io.norm[e].y;
+        } else {
+            m = io.in_lse[2 * e], l2s = io.in_lse[2 * e + 1] * kLog2e;
+            if (g.y != 0.f) H = io.in_entropy[e];
+        }
+        const RowCoef k = coef_of(m, m == -INFINITY ? 0.f : 1.f, l2s, H, g.x, g.y);
+        if (k.zero != 0.f) {
+            for (int c = i0 + gl; c < i1; c += L) x[c] = 0.f;
+            continue;
+        }
+        const auto each = [&](auto ent) {
+            constexpr bool ENT = decltype(ent)::value;
+            if constexpr (L == 64) {
+                for_vectors(x, w.tile, i0, i1, w.lane, [&](int from, float (&f)[4]) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) f[j] = grad_of<ENT>(k, f[j]);
+                    put_vector(x, from, i0, i1, f);
+                });
+            } else {
+                for (int c = i0 + gl; c < i1; c += 4 * L) {
+                    float f[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) f[j] = grad_of<ENT>(k, x[min(c + j * L, i1 - 1)]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (c + j * L < i1) x[c + j * L] = f[j];
+                }
+            }
+        };
+        if (k.e != 0.f) each(std::true_type());
+        else each(std::false_type());
+        const int act = min(max(w.item[p].act, i0), i1 - 1);
+        if (gl == 0) x[act] += k.g;  // behind the group's writes: LDS serves a wave in order
+    }
+}
+
 template <typename T, int MODE>
 __global__ __launch_bounds__(kThreads) void k_types(Rows q, TypesShape sh, TypesIO io) {
     constexpr int N = kVec<T>;
@@ -1029,64 +1149,26 @@ __global__ __launch_bounds__(kThreads) void k_types(Rows q, TypesShape sh, Types
         if (lane <= ns) off[lane] = my_off;
         if (lane < ns) order[lane] = my_order;
         wave_sync();
-        if (!kGradOnly) {
+        const WaveTile wt{tile, zs, item, row, off, ns, a, lane};
+        const auto for_classes = [&](const TypesShape &s, auto f) {
 #pragma unroll 1
-          for (int cl = 0; cl < 2; ++cl) {
-            const TypesClass tc = sh.cls[cl];
-            const int L = tc.lanes, gl = lane & (L - 1), gn = 64 / L;
-            for (int w0 = lane / L; w0 < n * tc.n; w0 += gn) {
-                const int ri = w0 * tc.magic >> 16, s = order[(cl ? sh.cls[0].n : 0) + w0 - ri * tc.n], p = ri * ns + s;
-                const int i0 = off[s], i1 = off[s + 1];
-                const float *x = zs + ri * a;
-                float m = -INFINITY;
-                if (L == 64) {
-                    for_vectors(x, tile, i0, i1, lane, [&](int, int, float (&f)[4]) { m = max_nan(max_nan(m, f[0]), max_nan(f[1], max_nan(f[2], f[3]))); });
-                } else {
-#pragma unroll 4
-                    for (int i = i0 + gl; i < i1; i += L) m = max_nan(m, x[i]);
-                }
-                m = group_reduce(m, L, -INFINITY, [](float b, float c) { return max_nan(b, c); });
-                const float ms = shift_of(m);
-                Sums sum{m, 0.f, 0.f};
-                const auto add_one = [&](float z1) {
-                    const float y = fmaxf((z1 - ms) * kLog2e, kYMin), e = exp2_hw(y);
-                    sum.s += e;
-                    sum.u = fmaf(e, y, sum.u);
-                };
-                if (L == 64) {
-                    for_vectors(x, tile, i0, i1, lane, [&](int, int, float (&f)[4]) {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) add_one(f[j]);
-                    });
-                } else {
-#pragma unroll 4
-                    for (int i = i0 + gl; i < i1; i += L) add_one(x[i]);
-                }
-                const auto add = [](float b, float c) { return b + c; };
-                sum.s = group_reduce(sum.s, L, 0.f, add);
-                sum.u = group_reduce(sum.u, L, 0.f, add);
-                if (!(m < INFINITY)) sum.s = sum.u = __builtin_nanf("");
-                if (gl != 0) continue;
-                const float zact = x[min(max(item[p].act, i0), i1 - 1)];
-                const LogSum l = log_sum_f32(sum);
-                const int64_t e = r0 * ns + p;
-                item[p].m = sum.s == 0.f ? -INFINITY : m;
-                item[p].l2s = l.l2s;
-                if (MODE == kTypesDiff) {  // long sums of small differences follow: 64 bits
-                    item[p].lp = log_prob(sum, zact);
-                    io.norm[e] = make_float2(sum.s == 0.f ? -INFINITY : m, l.l2s);
-                    continue;
-                }
-                const float H = entropy_f32(sum, l);
-                item[p].lp = (double)log_prob_f32(sum, l, zact);
-                item[p].H = H;
-                if (MODE == kTypesLogp && io.entropy) io.entropy[e] = H;
-                if (MODE == kTypesLogp && io.lse) {
-                    io.lse[2 * e] = m;
-                    io.lse[2 * e + 1] = sum.s == 0.f ? 0.f : l.ls;
+            for (int c = 0; c < 2; ++c) {
+                const TypesClass tc = s.cls[c];
+                const int *segs = order + (c ? s.cls[0].n : 0);
+                if (tc.n == 0) break;
+                switch (tc.lanes) {
+                    case 1: f(std::integral_constant<int, 1>(), tc, segs); break;
+                    case 2: f(std::integral_constant<int, 2>(), tc, segs); break;
+                    case 4: f(std::integral_constant<int, 4>(), tc, segs); break;
+                    case 8: f(std::integral_constant<int, 8>(), tc, segs); break;
+                    case 16: f(std::integral_constant<int, 16>(), tc, segs); break;
+                    case 32: f(std::integral_constant<int, 32>(), tc, segs); break;
+                    default: f(std::integral_constant<int, 64>(), tc, segs); break;
                 }
             }
-          }
+        };
+        if (!kGradOnly) {
+            for_classes(sh, [&](auto L, const TypesClass &tc, const int *segs) { types_sums<decltype(L)::value, MODE>(wt, io, tc, segs, r0, n); });
             wave_sync();
         }
         if (own) {
@@ -1115,53 +1197,7 @@ __global__ __launch_bounds__(kThreads) void k_types(Rows q, TypesShape sh, Types
         }
         wave_sync();
         if (MODE == kTypesLogp || MODE == kTypesDiff || !io.dz) continue;
-#pragma unroll 1
-        for (int cl = 0; cl < 2; ++cl) {
-          const TypesClass tc = sh.cls[cl];
-          const int L = tc.lanes, gl = lane & (L - 1), gn = 64 / L;
-          for (int w0 = lane / L; w0 < n * tc.n; w0 += gn) {
-            const int ri = w0 * tc.magic >> 16, s = order[(cl ? sh.cls[0].n : 0) + w0 - ri * tc.n], p = ri * ns + s;
-            const int i0 = off[s], i1 = off[s + 1];
-            const int64_t e = r0 * ns + p;
-            float *x = zs + ri * a;
-            const float2 g = row[ri];
-            float m, l2s, H = 0.f;
-            if (MODE == kTypesLoss) {
-                m = item[p].m, l2s = item[p].l2s, H = item[p].H;
-            } else if (MODE == kTypesGradPairs) {
-                m = -INFINITY, l2s = 0.f;
-                if (g.x != 0.f) m = io.norm[e].x, l2s = io.norm[e].y;
-            } else {
-                m = io.in_lse[2 * e], l2s = io.in_lse[2 * e + 1] * kLog2e;
-                if (g.y != 0.f) H = io.in_entropy[e];
-            }
-            const RowCoef k = coef_of(m, m == -INFINITY ? 0.f : 1.f, l2s, H, g.x, g.y);
-            if (k.zero != 0.f) {
-                for (int i = i0 + gl; i < i1; i += L) x[i] = 0.f;
-                continue;
-            }
-            const int act = min(max(item[p].act, i0), i1 - 1);
-            if (L == 64) {
-                for_vectors(x, tile, i0, i1, lane, [&](int from, int to, float (&f)[4]) {
-                    if (k.e != 0.f) {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) f[j] = grad_of<true>(k, f[j]);
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) f[j] = grad_of<false>(k, f[j]);
-                    }
-                    put_vector(x, from, to, i0, i1, f);
-                });
-            } else if (k.e != 0.f) {
-#pragma unroll 4
-                for (int i = i0 + gl; i < i1; i += L) x[i] = grad_of<true>(k, x[i]);
-            } else {
-#pragma unroll 4
-                for (int i = i0 + gl; i < i1; i += L) x[i] = grad_of<false>(k, x[i]);
-            }
-            if (gl == 0) x[act] += k.g;  // behind the group's writes: LDS serves a wave in order
-          }
-        }
+        for_classes(sh, [&](auto L, const TypesClass &tc, const int *segs) { types_grads<decltype(L)::value, MODE>(wt, io, tc, segs, r0, n); });
         wave_sync();
         store_tile<T>(static_cast<T *>(io.dz) + r0 * io.ld_d, io.ld_d, a, n, sh.magic, head, zs, lane);
         wave_sync();
