@@ -143,6 +143,23 @@ struct Parts {
     }
 };
 
+// A row's vectors as TPR-wide slices through buffer descriptors: thread t's vector of slice j lies at byte
+// 16 t of the slice, and the descriptor ends with the row (loads beyond give 0, stores go nowhere), so that
+// loads and stores need neither masks nor an address of their own a vector.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t slice(const void *base, int bytes, int from) {
+    char *p = static_cast<char *>(const_cast<void *>(base)) + from;
+    return __builtin_amdgcn_make_buffer_rsrc(p, 0, max(bytes - from, 0), 0x00027000);
+}
+__device__ __forceinline__ uint4 load_vec(__amdgpu_buffer_rsrc_t b, int byte) {
+    const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(b, byte, 0, 0);
+    return make_uint4(v.x, v.y, v.z, v.w);
+}
+__device__ __forceinline__ void put_vec(__amdgpu_buffer_rsrc_t b, int byte, const uint4 &v) {
+    __builtin_amdgcn_raw_buffer_store_b128(u32x4{v.x, v.y, v.z, v.w}, b, byte, 0, 0);
+}
+
 // Running sums of one lane, wave or workgroup relative to its own largest value.
 struct Sums {
     float m, s, u;
@@ -150,27 +167,51 @@ struct Sums {
 
 __device__ __forceinline__ float shift_of(float m) { return m == -INFINITY ? 0.f : m; }
 
+// y = (x - m) log2 e of a difference d = x - m.  With U (u is summed) log2 e is one fp32 number, whose error
+// log_sum mends from u; without, it is two and nothing is left to mend.
+template <bool U>
+__device__ __forceinline__ float to_base2(float d) {
+    return U ? d * kLog2e : fmaf(d, (float)kLog2eRest, d * kLog2e);
+}
+
 // Moves the sums to a larger maximum (its shift ms = shift_of(m_new)).
+template <bool U = true>
 __device__ __forceinline__ void rescale(Sums &q, float m_new, float ms) {
-    const float d = (q.m - ms) * kLog2e, f = exp2_hw(d);
-    q.u = f * (q.u + q.s * fmaxf(d, -1e4f));
+    const float d = to_base2<U>(q.m - ms), f = exp2_hw(d);
+    if (U) q.u = f * (q.u + q.s * fmaxf(d, -1e4f));
     q.s *= f;
     q.m = m_new;
 }
 
-template <int N>
-__device__ __forceinline__ void add_values(Sums &q, const float (&x)[N]) {
-    float gm = x[0];
+// Adds NV vectors or single values to a lane's sums, with one change of the maximum.
+template <bool U, int NV, int N>
+__device__ __forceinline__ void add_values(Sums &q, const float (&x)[NV][N]) {
+    float gm = -INFINITY;
 #pragma unroll
-    for (int i = 1; i < N; ++i) gm = max_nan(gm, x[i]);
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int i = 0; i < N; ++i) gm = max_nan(gm, x[j][i]);
     const float m = max_nan(q.m, gm), ms = shift_of(m);
-    rescale(q, m, ms);
+    rescale<U>(q, m, ms);
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const float y = fmaxf((x[i] - ms) * kLog2e, kYMin), e = exp2_hw(y);
-        q.s += e;
-        q.u = fmaf(e, y, q.u);
-    }
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (U) {
+                const float y = fmaxf(to_base2<U>(x[j][i] - ms), kYMin), e = exp2_hw(y);
+                q.s += e;
+                q.u = fmaf(e, y, q.u);
+            } else {
+                q.s += exp2_hw(to_base2<U>(x[j][i] - ms));
+            }
+        }
+}
+template <bool U, int N, int NV>
+__device__ __forceinline__ void add_vectors(Sums &q, const uint4 *raw) {
+    float x[NV][N];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) unpack(raw[j], x[j]);
+    add_values<U, NV, N>(q, x);
 }
 
 // Reductions over the first W lanes of a wave (W a power of two up to 64); the result in every lane.
@@ -188,12 +229,12 @@ __device__ __forceinline__ float lanes_reduce(float x, float none, Op op) {
     if constexpr (W > 32) x = op(x, dpp<0x143, 0xc>(x, none));  // row_bcast:31 into rows 2 and 3
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), W - 1));
 }
-template <int W>
+template <int W, bool U = true>
 __device__ __forceinline__ Sums lanes_join(Sums q) {
     const float m = lanes_reduce<W>(q.m, -INFINITY, [](float a, float b) { return max_nan(a, b); });
-    rescale(q, m, shift_of(m));
+    rescale<U>(q, m, shift_of(m));
     const auto add = [](float a, float b) { return a + b; };
-    return Sums{m, lanes_reduce<W>(q.s, 0.f, add), lanes_reduce<W>(q.u, 0.f, add)};
+    return Sums{m, lanes_reduce<W>(q.s, 0.f, add), U ? lanes_reduce<W>(q.u, 0.f, add) : 0.f};
 }
 
 // Sum of 64 bits over a wave, in lane order by pairs; the result in every lane.
@@ -212,14 +253,14 @@ __device__ __forceinline__ double wave_sum(double x) {
 
 // The sums of a row from those of its TPR threads, in every thread.  `red` has 2 halves of TPR / 64
 // entries, used in turn, so that one barrier a row is enough.
-template <int TPR>
+template <int TPR, bool U = true>
 __device__ __forceinline__ Sums row_join(Sums q, Sums (*red)[16], int &half) {
-    q = lanes_join<64>(q);
+    q = lanes_join<64, U>(q);
     if constexpr (TPR > 64) {
         constexpr int W = TPR / 64;
         if (threadIdx.x % 64 == 0) red[half][threadIdx.x / 64] = q;
         __syncthreads();
-        q = lanes_join<W>(red[half][threadIdx.x % W]);
+        q = lanes_join<W, U>(red[half][threadIdx.x % W]);
         half ^= 1;
     }
     // NaN or +inf among the values: everything that follows is NaN
@@ -278,17 +319,20 @@ __device__ __forceinline__ float grad_any(const RowCoef &k, float z) {
     return k.e != 0.f ? grad_of<true>(k, z) : grad_of<false>(k, z);
 }
 
-// One vector's gradient to column i0 of the row dz; `same`: dz has the logits' alignment.
-template <typename T>
+// One vector's gradient to column i0 of the row dz; `same`: dz has the logits' alignment; STREAM: past the caches.
+template <typename T, bool STREAM>
 __device__ __forceinline__ void store_vec(T *dz, int i0, const float (&x)[kVec<T>], bool same) {
     if (same) {
-        *reinterpret_cast<uint4 *>(dz + i0) = pack(x);
+        const uint4 v = pack(x);
+        u32x4 *to = reinterpret_cast<u32x4 *>(dz + i0);
+        if (STREAM) __builtin_nontemporal_store(u32x4{v.x, v.y, v.z, v.w}, to);
+        else *to = u32x4{v.x, v.y, v.z, v.w};
     } else {
 #pragma unroll
         for (int i = 0; i < kVec<T>; ++i) store(dz + i0 + i, x[i]);
     }
 }
-template <typename T>
+template <typename T, bool STREAM>
 __device__ __forceinline__ void grad_vec(T *dz, int i0, const uint4 &raw, const RowCoef &k, bool same) {
     float x[kVec<T>];
     unpack(raw, x);
@@ -302,14 +346,14 @@ __device__ __forceinline__ void grad_vec(T *dz, int i0, const uint4 &raw, const 
 #pragma unroll
         for (int i = 0; i < kVec<T>; ++i) x[i] = grad_of<false>(k, x[i]);
     }
-    store_vec<T>(dz, i0, x, same);
+    store_vec<T, STREAM>(dz, i0, x, same);
 }
 
 // ---- statistics of (row, chunk) items: a chunk is `per` vectors, the first also has the row's edges ----
-enum Out : int { kPartial = 0, kLogp = 1 };
+enum Out : int { kPartial = 0, kLogp = 1, kPartialLogp = 2 };
 
 struct StatOut {
-    Stat *stat;  // kPartial: [row][chunk] {m, s, u, z[action]}
+    Stat *stat;  // kPartial: [row][chunk] {m, s, u, z[action]}; kPartialLogp: without u
     float *logp, *entropy, *lse;
 };
 
@@ -325,50 +369,55 @@ __device__ __forceinline__ void put_logp(const StatOut &o, int64_t r, const Sums
 
 template <typename T, int TPR, int NV, int OUT>
 __global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void k_stats(Rows q, int chunks, int per, StatOut o) {
-    constexpr int WG = TPR < kThreads ? kThreads : TPR, N = kVec<T>;
+    constexpr int WG = TPR < kThreads ? kThreads : TPR, N = kVec<T>, G = NV < 4 ? NV : 4;
+    constexpr bool U = OUT != kPartialLogp;
     __shared__ Sums red[2][16];
     int half = 0;
     const int t = threadIdx.x % TPR;
     const int64_t items = (int64_t)q.M * chunks;
     for (int64_t it = (int64_t)blockIdx.x * (WG / TPR) + threadIdx.x / TPR; it < items; it += (int64_t)gridDim.x * (WG / TPR)) {
-        const int r = chunks == 1 ? (int)it : (int)((uint32_t)it / (uint32_t)chunks), c = (int)(it - (int64_t)r * chunks);
+        // a wave lies in one item
+        const int r = __builtin_amdgcn_readfirstlane(chunks == 1 ? (int)it : (int)(it / chunks));
+        const int c = __builtin_amdgcn_readfirstlane((int)(it - (int64_t)r * chunks));
         if (!row_counts(q, r)) continue;
         const T *z = static_cast<const T *>(q.z) + (int64_t)r * q.ld;
         const Parts<T> parts(z, q.a);
         const int act = min(max(q.act[r], 0), q.a - 1);
         const float zact = to_f32(z[act]);
+        const int ei = c == 0 ? parts.edge(t) : -1;
+        const float ex = ei < 0 ? -INFINITY : to_f32(z[ei]);
         Sums sum{-INFINITY, 0.f, 0.f};
         const int v1 = min((c + 1) * per, parts.full);
-        const T *body = z + parts.head;
-        for (int v = c * per + t; v < v1; v += TPR * NV) {
+        for (int v = c * per; v < v1; v += TPR * NV) {
+            const T *from = z + parts.head + (int64_t)v * N;
+            const int left = v1 - v;
             uint4 raw[NV];
 #pragma unroll
-            for (int j = 0; j < NV; ++j)
-                raw[j] = v + TPR * j < v1 ? *reinterpret_cast<const uint4 *>(body + (int64_t)(v + TPR * j) * N) : all_excluded<T>();
+            for (int j = 0; j < NV; ++j) raw[j] = load_vec(slice(from, left * 16, TPR * 16 * j), t * 16);
 #pragma unroll
-            for (int j = 0; j < NV; ++j) {
-                float x[N];
-                unpack(raw[j], x);
-                add_values<N>(sum, x);
+            for (int g = 0; g < NV; g += G) {
+                if (TPR * g >= left) break;
+#pragma unroll
+                for (int j = g; j < g + G; ++j)
+                    if (TPR * (j + 1) > left && t + TPR * j >= left) raw[j] = all_excluded<T>();
+                add_vectors<U, N, G>(sum, raw + g);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
         if (c == 0 && parts.head + parts.tail > 0) {
-            const int i = parts.edge(t);
-            const float x[1] = {i < 0 ? -INFINITY : to_f32(z[i])};
-            add_values<1>(sum, x);
+            const float x[1][1] = {{ex}};
+            add_values<U, 1, 1>(sum, x);
         }
-        sum = row_join<TPR>(sum, red, half);
+        sum = row_join<TPR, U>(sum, red, half);
         if (t == 0) {
-            if (OUT == kPartial) {
-                o.stat[it] = Stat{sum.m, sum.s, sum.u, zact};
-            } else {
-                put_logp(o, r, sum, zact);
-            }
+            if (OUT == kLogp) put_logp(o, r, sum, zact);
+            else o.stat[it] = Stat{sum.m, sum.s, sum.u, zact};
         }
     }
 }
 
 // A row's sums from its chunks', by one thread in chunk order, eight loads in flight.
+template <bool U = true>
 __device__ __forceinline__ Sums join_chunks(const Stat *__restrict__ st, int chunks) {
     if (chunks == 1) return Sums{st[0].m, st[0].s, st[0].u};
     Sums q{-INFINITY, 0.f, 0.f};
@@ -380,11 +429,11 @@ __device__ __forceinline__ Sums join_chunks(const Stat *__restrict__ st, int chu
 #pragma unroll
         for (int j = 0; j < 8; ++j) m = max_nan(m, x[j].m);
         const float ms = shift_of(m);
-        rescale(q, m, ms);
+        rescale<U>(q, m, ms);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             Sums y{x[j].m, x[j].s, x[j].u};
-            rescale(y, m, ms);
+            rescale<U>(y, m, ms);
             if (c + j < chunks) {
                 q.s += y.s;
                 q.u += y.u;
@@ -430,23 +479,6 @@ __device__ __forceinline__ void loss_grad(const LossArgs &a, float w, float old,
     surrogate = s2 < s1 ? s2 : s1;
     gl = w * (ds + dk);
     ge = -w * a.w_entropy;
-}
-
-// A row's vectors as TPR-wide slices through buffer descriptors: thread t's vector of slice j lies at byte
-// 16 t of the slice, and the descriptor ends with the row (loads beyond give 0, stores go nowhere), so that
-// loads and stores need neither masks nor an address of their own a vector.
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t slice(const void *base, int bytes, int from) {
-    char *p = static_cast<char *>(const_cast<void *>(base)) + from;
-    return __builtin_amdgcn_make_buffer_rsrc(p, 0, max(bytes - from, 0), 0x00027000);
-}
-__device__ __forceinline__ uint4 load_vec(__amdgpu_buffer_rsrc_t b, int byte) {
-    const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(b, byte, 0, 0);
-    return make_uint4(v.x, v.y, v.z, v.w);
-}
-__device__ __forceinline__ void put_vec(__amdgpu_buffer_rsrc_t b, int byte, const uint4 &v) {
-    __builtin_amdgcn_raw_buffer_store_b128(u32x4{v.x, v.y, v.z, v.w}, b, byte, 0, 0);
 }
 
 // The whole row dz = 0, or (other alignment than the logits') an element at a time from memory.
@@ -510,19 +542,14 @@ __global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void k_loss(Rows q
         for (int j = 0; j < NV; ++j) {
             if (TPR * j >= full) continue;  // uniform
             if (TPR * (j + 1) > full && t + TPR * j >= full) raw[j] = all_excluded<T>();
-            float x[N];
-            unpack(raw[j], x);
-            add_values<N>(sum, x);
+            add_vectors<true, N, 1>(sum, raw + j);
             __builtin_amdgcn_sched_barrier(0);
         }
-        for (int v = t + TPR * NV; v < full; v += TPR) {  // what the registers do not hold
-            float x[N];
-            unpack(reinterpret_cast<const uint4 *>(body)[v], x);
-            add_values<N>(sum, x);
-        }
+        for (int v = t + TPR * NV; v < full; v += TPR)  // what the registers do not hold
+            add_vectors<true, N, 1>(sum, reinterpret_cast<const uint4 *>(body) + v);
         if (parts.head + parts.tail > 0) {
-            const float x[1] = {ex};
-            add_values<1>(sum, x);
+            const float x[1][1] = {{ex}};
+            add_values<true, 1, 1>(sum, x);
         }
         sum = row_join<TPR>(sum, red, half);
         const LogSum l = log_sum_f32(sum);
@@ -546,7 +573,7 @@ __global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void k_loss(Rows q
         if (k.e != 0.f) grad_slices<T, TPR, NV, true>(dz + parts.head, full, raw, k, t);
         else grad_slices<T, TPR, NV, false>(dz + parts.head, full, raw, k, t);
         for (int v = t + TPR * NV; v < full; v += TPR)
-            grad_vec<T>(dz, parts.head + v * N, reinterpret_cast<const uint4 *>(body)[v], k, true);
+            grad_vec<T, false>(dz, parts.head + v * N, reinterpret_cast<const uint4 *>(body)[v], k, true);
         if (ei >= 0) store(dz + ei, grad_any(k, ex));
         // the chosen action's column once more, by the thread that wrote it
         const int av = (act - parts.head) / N;
@@ -613,17 +640,18 @@ struct PairArgs {
 // Pair p by workgroup p (stepping over pairs): both tracks' log ratios, the loss terms and every row's
 // gradient.  Rows come as `chunks` parts of statistics (one segment; their results go to fin) or as
 // weighted log ratios `diff` (several; their gradients go to g_row).
-__global__ __launch_bounds__(kThreads) void k_pairs(PairArgs a, const Stat *__restrict__ stat, const double *__restrict__ diff,
+template <int WG>
+__global__ __launch_bounds__(WG) void k_pairs(PairArgs a, const Stat *__restrict__ stat, const double *__restrict__ diff,
                                                     RowFin *__restrict__ fin, float *__restrict__ g_row,
                                                     double *__restrict__ terms, float *__restrict__ ratio) {
-    __shared__ double part[2][2][kThreads / 64];
+    __shared__ double part[2][2][WG / 64];
     int half = 0;
     for (int64_t p = blockIdx.x; p < a.n_pairs; p += gridDim.x) {
         // in order these are one run of rows, the rejected track's behind the preferred one's
         const int lo = clamp_row(a.seq_ptr[2 * p], a.n_rows), mid = clamp_row(a.seq_ptr[2 * p + 1], a.n_rows);
         const int hi = clamp_row(a.seq_ptr[2 * p + 2], a.n_rows);
         double s[2] = {0.0, 0.0};
-        for (int64_t r = (int64_t)lo + threadIdx.x; r < hi; r += kThreads) {
+        for (int64_t r = (int64_t)lo + threadIdx.x; r < hi; r += WG) {
             double d;
             if (diff) {
                 d = diff[r];
@@ -631,8 +659,9 @@ __global__ __launch_bounds__(kThreads) void k_pairs(PairArgs a, const Stat *__re
                 const float w = a.weight ? a.weight[r] : 1.f;
                 if (w == 0.f) continue;
                 const float ref = a.logp_ref ? a.logp_ref[r] : 0.f;
-                const Sums q = join_chunks(stat + r * a.chunks, a.chunks);
-                d = (double)w * (log_prob(q, stat[r * a.chunks].zact) - (double)ref);
+                const Sums q = join_chunks<false>(stat + r * a.chunks, a.chunks);
+                const double lp = q.s == 0.f ? 0.0 : ((double)stat[r * a.chunks].zact - (double)q.m) - log((double)q.s);
+                d = (double)w * (lp - (double)ref);
                 if (fin) {
                     fin[r].m = q.s == 0.f ? -INFINITY : q.m;
                     fin[r].l2s = __builtin_amdgcn_logf(q.s);
@@ -648,7 +677,7 @@ __global__ __launch_bounds__(kThreads) void k_pairs(PairArgs a, const Stat *__re
         double R[2];
         for (int side = 0; side < 2; ++side) {
             R[side] = part[half][side][0];
-            for (int i = 1; i < kThreads / 64; ++i) R[side] += part[half][side][i];
+            for (int i = 1; i < WG / 64; ++i) R[side] += part[half][side][i];
         }
         half ^= 1;  // the next pair's sums go to the other half: one barrier a pair
         const double h = (double)a.beta * (R[0] - R[1]);
@@ -668,7 +697,7 @@ __global__ __launch_bounds__(kThreads) void k_pairs(PairArgs a, const Stat *__re
         }
         if (!fin && !g_row) continue;
         const double g = (double)a.beta * ((double)a.smoothing - down) / (double)a.n_pairs;
-        for (int64_t r = (int64_t)lo + threadIdx.x; r < hi; r += kThreads) {
+        for (int64_t r = (int64_t)lo + threadIdx.x; r < hi; r += WG) {
             const float w = a.weight ? a.weight[r] : 1.f;
             const float gr = w == 0.f ? 0.f : (float)((double)w * (r >= mid ? -g : g));
             if (fin) fin[r].g = gr;
@@ -755,7 +784,7 @@ __device__ void loss_of_rows(const GradSrc &a, int M) {
     }
 }
 
-template <typename T, int SRC>
+template <typename T, int SRC, bool STREAM>
 __global__ __launch_bounds__(kThreads) void k_grad(Rows q, int chunks, int per, GradSrc a) {
     constexpr int N = kVec<T>, NV = 4;
     const int64_t items = (int64_t)q.M * chunks;
@@ -804,7 +833,7 @@ __global__ __launch_bounds__(kThreads) void k_grad(Rows q, int chunks, int per, 
             if (k.zero == 0.f) {
 #pragma unroll
                 for (int j = 0; j < NV; ++j)
-                    if (v + kThreads * j < v1) raw[j] = *reinterpret_cast<const uint4 *>(body + (int64_t)(v + kThreads * j) * N);
+                    if (v + kThreads * j < v1) raw[j] = reinterpret_cast<const uint4 *>(body)[v + kThreads * j];
             }
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
@@ -813,7 +842,7 @@ __global__ __launch_bounds__(kThreads) void k_grad(Rows q, int chunks, int per, 
                 // kFromFin and kFromLse: the chosen action's logit lies in its own vector
                 float za = 0.f;
                 if (SRC != kFromLoss && vj == av && k.zero == 0.f) za = to_f32(z[act]);
-                grad_vec<T>(dz, parts.head + vj * N, raw[j], k, same);
+                grad_vec<T, STREAM>(dz, parts.head + vj * N, raw[j], k, same);
                 if (vj == av && k.zero == 0.f) store(dz + act, SRC == kFromLoss ? hot : grad_any(k, za) + k.g);
             }
         }
@@ -1238,12 +1267,19 @@ int vec_of(const harl_policy_head *h) { return h->dtype == HARL_BF16 ? 8 : 4; }
 constexpr int kSplitItems = 1024;  // items that a launch of few rows is cut into
 constexpr int kMaxChunks = 64;     // a wave joins a row's chunks
 constexpr int kLossGrid = 8192;    // workgroups of k_loss: its terms
+constexpr int kPrefChunk = 2048;   // vectors of a preference row's chunk at most
 
 // Chunks of a row: rows that leave the machine idle are cut until there are about kSplitItems items, none of
 // fewer than 512 vectors (two a thread).
 int chunks_for(const harl_policy_head *h, int32_t M) {
     const int64_t vecs = h->a / vec_of(h);
     return (int)std::max<int64_t>(1, std::min<int64_t>({ceil_div(kSplitItems, M), (int64_t)kMaxChunks, vecs / 512}));
+}
+
+// The preference loss joins a row's chunks anyway, so all its rows are cut: whole rows of 8,192 vectors
+// leave the machine half empty in the last of two rounds.
+int pref_chunks_for(const harl_policy_head *h, int32_t M) {
+    return (int)std::min<int64_t>(kMaxChunks, std::max<int64_t>(chunks_for(h, M), ceil_div(h->a / vec_of(h), kPrefChunk)));
 }
 
 template <typename T, int OUT>
@@ -1253,7 +1289,7 @@ void launch_stats_as(const Rows &q, int chunks, const StatOut &o, hipStream_t st
     if (chunks == 1 && q.a / kVec<T> <= 512)  // a wave a row: no barrier, four rows a workgroup
         hipLaunchKernelGGL((k_stats<T, 64, 4, OUT>), dim3(grid_for(ceil_div(items, 4))), dim3(kThreads), 0, stream, q, chunks, per, o);
     else
-        hipLaunchKernelGGL((k_stats<T, 256, 4, OUT>), dim3(grid_for(items)), dim3(kThreads), 0, stream, q, chunks, per, o);
+        hipLaunchKernelGGL((k_stats<T, 256, 8, OUT>), dim3(grid_for(items)), dim3(kThreads), 0, stream, q, chunks, per, o);
 }
 
 template <int OUT>
@@ -1269,10 +1305,13 @@ int launch_wide_grad(const harl_policy_head *h, const Rows &q, const GradSrc &a,
     const int vecs = std::max(h->a / vec_of(h), 1);
     const int chunks = (int)ceil_div(vecs, 1024), per = (int)ceil_div(vecs, chunks);
     const unsigned grid = (a.dz ? grid_for((int64_t)q.M * chunks) : 0) + (SRC == kFromLse ? 0 : 1);
-    if (h->dtype == HARL_BF16)
-        hipLaunchKernelGGL((k_grad<uint16_t, SRC>), dim3(grid), dim3(kThreads), 0, stream, q, chunks, per, a);
-    else
-        hipLaunchKernelGGL((k_grad<float, SRC>), dim3(grid), dim3(kThreads), 0, stream, q, chunks, per, a);
+    // A large gradient that stays in the caches is written back while the next pass reads its logits: 134 MB
+    // take 84 us with it and 74 past them, 500 MB 254 and 229; 42 MB the same either way.
+    const bool past = SRC != kFromLoss && (int64_t)q.M * h->a * (h->dtype == HARL_BF16 ? 2 : 4) > ((int64_t)64 << 20);
+    constexpr bool kPast = SRC != kFromLoss;
+    const auto kernel = h->dtype == HARL_BF16 ? (past ? k_grad<uint16_t, SRC, kPast> : k_grad<uint16_t, SRC, false>)
+                                              : (past ? k_grad<float, SRC, kPast> : k_grad<float, SRC, false>);
+    hipLaunchKernelGGL(kernel, dim3(grid), dim3(kThreads), 0, stream, q, chunks, per, a);
     HARL_HIP_CHECK(hipGetLastError());
     return HARL_OK;
 }
@@ -1400,7 +1439,8 @@ Ws loss_ws(const harl_policy_head *h, int64_t M, char *base) {
                               3 * std::min<int64_t>(M, kLossGrid)}, base);
 }
 Ws preference_ws(const harl_policy_head *h, int64_t rows, int64_t pairs, char *base) {
-    return ws_layout(h->n_seg == 1 ? WsCounts{rows + kSplitItems, rows, 0, 0, 4 * pairs}
+    const int64_t cut = std::min<int64_t>(kMaxChunks, std::max<int64_t>(1, ceil_div(h->a / vec_of(h), kPrefChunk)));
+    return ws_layout(h->n_seg == 1 ? WsCounts{rows * cut + kSplitItems, rows, 0, 0, 4 * pairs}
                                    : WsCounts{0, 0, rows, rows * h->n_seg, 4 * pairs}, base);
 }
 
@@ -1511,7 +1551,7 @@ int preference_loss_launch(const harl_policy_head *head, const harl_preference_c
     q.seq_ptr = seq_ptr;
     q.n_seq = 2 * n_pairs;
     const bool grad = dlogits && n_rows > 0, types = head->n_seg > 1;
-    const int chunks = !types && n_rows > 0 ? chunks_for(head, n_rows) : 1;
+    const int chunks = !types && n_rows > 0 ? pref_chunks_for(head, n_rows) : 1;
     if (n_rows > 0 && types) {
         TypesIO io{};
         io.logp_ref = logp_ref;
@@ -1520,10 +1560,13 @@ int preference_loss_launch(const harl_policy_head *head, const harl_preference_c
         if (const int rc = launch_types<kTypesDiff>(head, q, io, stream)) return rc;
     } else if (n_rows > 0) {
         const StatOut o{w.stat, nullptr, nullptr, nullptr};
-        if (const int rc = launch_wide_stats<kPartial>(head, q, chunks, o, stream)) return rc;
+        if (const int rc = launch_wide_stats<kPartialLogp>(head, q, chunks, o, stream)) return rc;
     }
     const PairArgs a{logp_ref, weight, seq_ptr, n_rows, chunks, n_pairs, cfg->beta, cfg->smoothing};
-    hipLaunchKernelGGL(k_pairs, dim3(grid_for(n_pairs)), dim3(kThreads), 0, stream, a, w.stat, types ? w.diff : nullptr,
+    // a thread a row of an average pair
+    const auto pairs = (int64_t)n_pairs * 256 < n_rows ? k_pairs<1024> : k_pairs<256>;
+    const unsigned pair_threads = (int64_t)n_pairs * 256 < n_rows ? 1024 : 256;
+    hipLaunchKernelGGL(pairs, dim3(grid_for(n_pairs)), dim3(pair_threads), 0, stream, a, w.stat, types ? w.diff : nullptr,
                        grad && !types ? w.fin : nullptr, grad && types ? w.g_row : nullptr, w.terms, ratio);
     HARL_HIP_CHECK(hipGetLastError());
     if (grad && types) {
