@@ -167,24 +167,16 @@ struct Sums {
 
 __device__ __forceinline__ float shift_of(float m) { return m == -INFINITY ? 0.f : m; }
 
-// y = (x - m) log2 e of a difference d = x - m.  With U (u is summed) log2 e is one fp32 number, whose error
-// log_sum mends from u; without, it is two and nothing is left to mend.
-template <bool U>
-__device__ __forceinline__ float to_base2(float d) {
-    return U ? d * kLog2e : fmaf(d, (float)kLog2eRest, d * kLog2e);
-}
-
 // Moves the sums to a larger maximum (its shift ms = shift_of(m_new)).
-template <bool U = true>
 __device__ __forceinline__ void rescale(Sums &q, float m_new, float ms) {
-    const float d = to_base2<U>(q.m - ms), f = exp2_hw(d);
-    if (U) q.u = f * (q.u + q.s * fmaxf(d, -1e4f));
+    const float d = (q.m - ms) * kLog2e, f = exp2_hw(d);
+    q.u = f * (q.u + q.s * fmaxf(d, -1e4f));
     q.s *= f;
     q.m = m_new;
 }
 
 // Adds NV vectors or single values to a lane's sums, with one change of the maximum.
-template <bool U, int NV, int N>
+template <int NV, int N>
 __device__ __forceinline__ void add_values(Sums &q, const float (&x)[NV][N]) {
     float gm = -INFINITY;
 #pragma unroll
@@ -192,26 +184,22 @@ __device__ __forceinline__ void add_values(Sums &q, const float (&x)[NV][N]) {
 #pragma unroll
         for (int i = 0; i < N; ++i) gm = max_nan(gm, x[j][i]);
     const float m = max_nan(q.m, gm), ms = shift_of(m);
-    rescale<U>(q, m, ms);
+    rescale(q, m, ms);
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            if (U) {
-                const float y = fmaxf(to_base2<U>(x[j][i] - ms), kYMin), e = exp2_hw(y);
-                q.s += e;
-                q.u = fmaf(e, y, q.u);
-            } else {
-                q.s += exp2_hw(to_base2<U>(x[j][i] - ms));
-            }
+            const float y = fmaxf((x[j][i] - ms) * kLog2e, kYMin), e = exp2_hw(y);
+            q.s += e;
+            q.u = fmaf(e, y, q.u);
         }
 }
-template <bool U, int N, int NV>
+template <int N, int NV>
 __device__ __forceinline__ void add_vectors(Sums &q, const uint4 *raw) {
     float x[NV][N];
 #pragma unroll
     for (int j = 0; j < NV; ++j) unpack(raw[j], x[j]);
-    add_values<U, NV, N>(q, x);
+    add_values<NV, N>(q, x);
 }
 
 // Reductions over the first W lanes of a wave (W a power of two up to 64); the result in every lane.
@@ -229,12 +217,12 @@ __device__ __forceinline__ float lanes_reduce(float x, float none, Op op) {
     if constexpr (W > 32) x = op(x, dpp<0x143, 0xc>(x, none));  // row_bcast:31 into rows 2 and 3
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), W - 1));
 }
-template <int W, bool U = true>
+template <int W>
 __device__ __forceinline__ Sums lanes_join(Sums q) {
     const float m = lanes_reduce<W>(q.m, -INFINITY, [](float a, float b) { return max_nan(a, b); });
-    rescale<U>(q, m, shift_of(m));
+    rescale(q, m, shift_of(m));
     const auto add = [](float a, float b) { return a + b; };
-    return Sums{m, lanes_reduce<W>(q.s, 0.f, add), U ? lanes_reduce<W>(q.u, 0.f, add) : 0.f};
+    return Sums{m, lanes_reduce<W>(q.s, 0.f, add), lanes_reduce<W>(q.u, 0.f, add)};
 }
 
 // Sum of 64 bits over a wave, in lane order by pairs; the result in every lane.
@@ -253,14 +241,14 @@ __device__ __forceinline__ double wave_sum(double x) {
 
 // The sums of a row from those of its TPR threads, in every thread.  `red` has 2 halves of TPR / 64
 // entries, used in turn, so that one barrier a row is enough.
-template <int TPR, bool U = true>
+template <int TPR>
 __device__ __forceinline__ Sums row_join(Sums q, Sums (*red)[16], int &half) {
-    q = lanes_join<64, U>(q);
+    q = lanes_join<64>(q);
     if constexpr (TPR > 64) {
         constexpr int W = TPR / 64;
         if (threadIdx.x % 64 == 0) red[half][threadIdx.x / 64] = q;
         __syncthreads();
-        q = lanes_join<W, U>(red[half][threadIdx.x % W]);
+        q = lanes_join<W>(red[half][threadIdx.x % W]);
         half ^= 1;
     }
     // NaN or +inf among the values: everything that follows is NaN
@@ -278,42 +266,42 @@ __device__ __forceinline__ double entropy_of(const Sums &q) {
     return q.s == 0.f ? 0.0 : log_sum(q) - kLn2d * (double)q.u / (double)q.s;
 }
 
-// The same in fp32, for what is rounded to fp32 next: log s and its error of log2 e.
+// The same in fp32, for what is rounded to fp32 next.  The hardware's log2 s is good to a step of its own size
+// (1.9e-6 for a vocabulary); s 2^-(that) - 1 is what it misses.
 struct LogSum {
-    float l2s, ls, mean_y;
+    float l2s, ls, mean_y, inv_s;
 };
 __device__ __forceinline__ LogSum log_sum_f32(const Sums &q) {
-    const float l2s = __builtin_amdgcn_logf(q.s), mean_y = q.u * __builtin_amdgcn_rcpf(q.s);
-    return LogSum{l2s, fmaf(l2s, kLn2, (float)(kLog2eRest * kLn2d * kLn2d) * mean_y), mean_y};
+    const float l2s = __builtin_amdgcn_logf(q.s), inv_s = 1.f / q.s, mean_y = q.u * inv_s;
+    const float missed = fmaf(q.s, exp2_hw(-l2s), -1.f);
+    return LogSum{l2s, fmaf(l2s, kLn2, fmaf((float)(kLog2eRest * kLn2d * kLn2d), mean_y, missed)), mean_y, inv_s};
 }
 __device__ __forceinline__ float log_prob_f32(const Sums &q, const LogSum &l, float zact) { return q.s == 0.f ? 0.f : (zact - q.m) - l.ls; }
 __device__ __forceinline__ float entropy_f32(const Sums &q, const LogSum &l) { return q.s == 0.f ? 0.f : l.ls - kLn2 * l.mean_y; }
 
-// What the gradient of a row is made of: dz_i = -p_i (g + h (y_i + shift of H)) and g more at the action,
-// p = 2^y, y = (z - m) log2 e - log2 s.  Written as p (c + e y): c = -(g_logp + g_H H), e = -g_H ln 2.
+// What the gradient of a row is made of: dz_i = -p_i (g_logp + g_H (log p_i + H)), and g_logp more at the
+// action.  With y = (z - m) log2 e, p = 2^y / s and log p = ln 2 (y - log2 s) it is 2^y (c + e y),
+//   e = -g_H ln 2 / s,  c = -(g_logp + g_H (H - ln 2 log2 s)) / s:
+// 1 / s is in the coefficients, not in the exponent, which would be rounded at its size.
 struct RowCoef {
-    float m, l2s, c, e, g, zero;  // zero != 0: the row's gradient is 0
+    float m, c, e, g, zero;  // zero != 0: the row's gradient is 0
 };
 
-__device__ __forceinline__ RowCoef coef_of(float m, float s, float l2s, float H, float gl, float ge) {
+// `empty`: no column has a probability.  rest: log s; used with the entropy's gradient only, as H.
+__device__ __forceinline__ RowCoef coef_of(float m, bool empty, float inv_s, float rest, float H, float gl, float ge) {
     RowCoef k;
     k.m = shift_of(m);
-    k.l2s = l2s;
-    k.c = -(gl + (ge != 0.f ? ge * H : 0.f));
-    k.e = -ge * kLn2;
+    k.c = -(gl + (ge != 0.f ? ge * (H - rest) : 0.f)) * inv_s;
+    k.e = -ge * kLn2 * inv_s;
     k.g = gl;
-    k.zero = s == 0.f || (gl == 0.f && ge == 0.f) ? 1.f : 0.f;
+    k.zero = empty || (gl == 0.f && ge == 0.f) ? 1.f : 0.f;
     return k;
 }
 
 template <bool ENT>
 __device__ __forceinline__ float grad_of(const RowCoef &k, float z) {
-    float y = fmaf(z - k.m, kLog2e, -k.l2s);
-    if constexpr (ENT) {
-        const float p = exp2_hw(y);
-        return p * fmaf(k.e, fmaxf(y, kYMin), k.c);
-    }
-    return exp2_hw(y) * k.c;
+    const float y = (z - k.m) * kLog2e, e = exp2_hw(y);
+    return ENT ? e * fmaf(k.e, fmaxf(y, kYMin), k.c) : e * k.c;
 }
 __device__ __forceinline__ float grad_any(const RowCoef &k, float z) {
     return k.e != 0.f ? grad_of<true>(k, z) : grad_of<false>(k, z);
@@ -350,10 +338,10 @@ __device__ __forceinline__ void grad_vec(T *dz, int i0, const uint4 &raw, const 
 }
 
 // ---- statistics of (row, chunk) items: a chunk is `per` vectors, the first also has the row's edges ----
-enum Out : int { kPartial = 0, kLogp = 1, kPartialLogp = 2 };
+enum Out : int { kPartial = 0, kLogp = 1 };
 
 struct StatOut {
-    Stat *stat;  // kPartial: [row][chunk] {m, s, u, z[action]}; kPartialLogp: without u
+    Stat *stat;  // kPartial: [row][chunk] {m, s, u, z[action]}
     float *logp, *entropy, *lse;
 };
 
@@ -370,7 +358,6 @@ __device__ __forceinline__ void put_logp(const StatOut &o, int64_t r, const Sums
 template <typename T, int TPR, int NV, int OUT>
 __global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void k_stats(Rows q, int chunks, int per, StatOut o) {
     constexpr int WG = TPR < kThreads ? kThreads : TPR, N = kVec<T>, G = NV < 4 ? NV : 4;
-    constexpr bool U = OUT != kPartialLogp;
     __shared__ Sums red[2][16];
     int half = 0;
     const int t = threadIdx.x % TPR;
@@ -400,15 +387,15 @@ __global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void k_stats(Rows 
 #pragma unroll
                 for (int j = g; j < g + G; ++j)
                     if (TPR * (j + 1) > left && t + TPR * j >= left) raw[j] = all_excluded<T>();
-                add_vectors<U, N, G>(sum, raw + g);
+                add_vectors<N, G>(sum, raw + g);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
         if (c == 0 && parts.head + parts.tail > 0) {
             const float x[1][1] = {{ex}};
-            add_values<U, 1, 1>(sum, x);
+            add_values<1, 1>(sum, x);
         }
-        sum = row_join<TPR, U>(sum, red, half);
+        sum = row_join<TPR>(sum, red, half);
         if (t == 0) {
             if (OUT == kLogp) put_logp(o, r, sum, zact);
             else o.stat[it] = Stat{sum.m, sum.s, sum.u, zact};
@@ -417,7 +404,6 @@ __global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void k_stats(Rows 
 }
 
 // A row's sums from its chunks', by one thread in chunk order, eight loads in flight.
-template <bool U = true>
 __device__ __forceinline__ Sums join_chunks(const Stat *__restrict__ st, int chunks) {
     if (chunks == 1) return Sums{st[0].m, st[0].s, st[0].u};
     Sums q{-INFINITY, 0.f, 0.f};
@@ -429,11 +415,11 @@ __device__ __forceinline__ Sums join_chunks(const Stat *__restrict__ st, int chu
 #pragma unroll
         for (int j = 0; j < 8; ++j) m = max_nan(m, x[j].m);
         const float ms = shift_of(m);
-        rescale<U>(q, m, ms);
+        rescale(q, m, ms);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             Sums y{x[j].m, x[j].s, x[j].u};
-            rescale<U>(y, m, ms);
+            rescale(y, m, ms);
             if (c + j < chunks) {
                 q.s += y.s;
                 q.u += y.u;
@@ -542,14 +528,14 @@ __global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void k_loss(Rows q
         for (int j = 0; j < NV; ++j) {
             if (TPR * j >= full) continue;  // uniform
             if (TPR * (j + 1) > full && t + TPR * j >= full) raw[j] = all_excluded<T>();
-            add_vectors<true, N, 1>(sum, raw + j);
+            add_vectors<N, 1>(sum, raw + j);
             __builtin_amdgcn_sched_barrier(0);
         }
         for (int v = t + TPR * NV; v < full; v += TPR)  // what the registers do not hold
-            add_vectors<true, N, 1>(sum, reinterpret_cast<const uint4 *>(body) + v);
+            add_vectors<N, 1>(sum, reinterpret_cast<const uint4 *>(body) + v);
         if (parts.head + parts.tail > 0) {
             const float x[1][1] = {{ex}};
-            add_values<true, 1, 1>(sum, x);
+            add_values<1, 1>(sum, x);
         }
         sum = row_join<TPR>(sum, red, half);
         const LogSum l = log_sum_f32(sum);
@@ -561,7 +547,7 @@ __global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void k_loss(Rows q
         acc[2] += (double)w * (double)H;
         if (t == 0 && o.logp) o.logp[r] = logp;
         if (!GRAD) continue;
-        const RowCoef k = coef_of(sum.m, sum.s, l.l2s, H, gl, ge);
+        const RowCoef k = coef_of(sum.m, sum.s == 0.f, l.inv_s, l.ls, H, gl, ge);
         if (k.zero != 0.f) {
             zero_row<T, TPR>(dz, q.a, t);
             continue;
@@ -625,9 +611,9 @@ __global__ __launch_bounds__(kThreads) void k_loss_sum(const double *__restrict_
 }
 
 // ---- preference loss ----
-// A row for the gradient pass of one segment: m, log2 s and the gradient of its log-probability.
+// A row for the gradient pass of one segment: m, 1 / s and the gradient of its log-probability.
 struct RowFin {
-    float m, l2s, g, pad;
+    float m, inv_s, g, pad;
 };
 
 struct PairArgs {
@@ -679,12 +665,11 @@ __global__ __launch_bounds__(WG) void k_pairs(PairArgs a, const Stat *__restrict
                 const float w = a.weight ? a.weight[r] : 1.f;
                 if (w == 0.f) continue;
                 const float ref = a.logp_ref ? a.logp_ref[r] : 0.f;
-                const Sums q = join_chunks<false>(stat + r * a.chunks, a.chunks);
-                const double lp = q.s == 0.f ? 0.0 : ((double)stat[r * a.chunks].zact - (double)q.m) - log((double)q.s);
-                d = (double)w * (lp - (double)ref);
+                const Sums q = join_chunks(stat + r * a.chunks, a.chunks);
+                d = (double)w * (log_prob(q, stat[r * a.chunks].zact) - (double)ref);
                 if (fin) {
                     fin[r].m = q.s == 0.f ? -INFINITY : q.m;
-                    fin[r].l2s = __builtin_amdgcn_logf(q.s);
+                    fin[r].inv_s = 1.f / q.s;
                 }
             }
             s[r >= mid ? 1 : 0] += d;
@@ -813,21 +798,22 @@ __global__ __launch_bounds__(kThreads) void k_grad(Rows q, int chunks, int per, 
         float hot = 0.f;  // the gradient at the action
         if (SRC == kFromFin) {
             const RowFin f = a.fin[r];
-            k = coef_of(f.m, f.m == -INFINITY ? 0.f : 1.f, f.l2s, 0.f, f.g, 0.f);
+            k = coef_of(f.m, f.m == -INFINITY, f.inv_s, 0.f, 0.f, f.g, 0.f);
         } else if (SRC == kFromLse) {
-            const float m = a.lse[2 * (int64_t)r], ge = a.g_entropy ? a.g_entropy[r] : 0.f;
-            k = coef_of(m, m == -INFINITY ? 0.f : 1.f, a.lse[2 * (int64_t)r + 1] * kLog2e, ge != 0.f ? a.entropy[r] : 0.f, a.g_logp[r], ge);
+            const float m = a.lse[2 * (int64_t)r], rest = a.lse[2 * (int64_t)r + 1], ge = a.g_entropy ? a.g_entropy[r] : 0.f;
+            k = coef_of(m, m == -INFINITY, exp2_hw(-rest * kLog2e), rest, ge != 0.f ? a.entropy[r] : 0.f, a.g_logp[r], ge);
         } else {
             const float w = a.loss.weight ? a.loss.weight[r] : a.loss.inv_m;
             k.zero = 1.f;
             if (w != 0.f) {
                 float zact;
                 const Sums s = join_wave(a.stat + (int64_t)r * a.stat_chunks, a.stat_chunks, zact);
-                const float H = (float)entropy_of(s), logp = (float)log_prob(s, zact);
+                const LogSum l = log_sum_f32(s);
+                const float H = entropy_f32(s, l), logp = log_prob_f32(s, l, zact);
                 float gl, ge, surrogate, kl;
                 loss_grad(a.loss, w, a.loss.logp_old[r], a.loss.logp_ref ? a.loss.logp_ref[r] : 0.f, a.loss.adv[r], logp, gl, ge,
                           surrogate, kl);
-                k = coef_of(s.m, s.s, __builtin_amdgcn_logf(s.s), H, gl, ge);
+                k = coef_of(s.m, s.s == 0.f, l.inv_s, l.ls, H, gl, ge);
                 hot = grad_any(k, zact) + k.g;
             }
         }
@@ -887,15 +873,15 @@ struct TypesShape {
 
 struct Item {
     double lp;
-    float m, l2s, H;  // m = -inf: an empty segment
-    int act;
+    float m, inv_s, H, ls;  // m = -inf: an empty segment; ls = log s
+    int act, pad;
 };
 
 struct TypesIO {
     float *logp, *entropy, *lse;                            // outputs (kTypesLogp; kTypesLoss: logp)
     const float *logp_ref;                                  // kTypesDiff
     double *diff;                                           // [row] weight (logp - logp_ref)
-    float2 *norm;                                           // [row][segment] {m, log2 s}: out of kTypesDiff, into kTypesGradPairs
+    float2 *norm;                                           // [row][segment] {m, 1 / s}: out of kTypesDiff, into kTypesGradPairs
     LossArgs loss;                                          // kTypesLoss
     double *terms;                                          // [workgroup][3]
     const float *in_lse, *in_entropy, *g_logp, *g_entropy;  // kTypesGradLse
@@ -1072,15 +1058,16 @@ __device__ __forceinline__ void types_sums(const WaveTile &w, const TypesIO &io,
         const LogSum l = log_sum_f32(sum);
         const int64_t e = r0 * w.ns + p;
         w.item[p].m = sum.s == 0.f ? -INFINITY : m;
-        w.item[p].l2s = l.l2s;
+        w.item[p].inv_s = l.inv_s;
         if (MODE == kTypesDiff || MODE == kTypesPairs) {  // long sums of small differences follow: 64 bits
             w.item[p].lp = log_prob(sum, zact);
-            if (MODE == kTypesDiff) io.norm[e] = make_float2(sum.s == 0.f ? -INFINITY : m, l.l2s);
+            if (MODE == kTypesDiff) io.norm[e] = make_float2(sum.s == 0.f ? -INFINITY : m, l.inv_s);
             continue;
         }
         const float H = entropy_f32(sum, l);
         w.item[p].lp = (double)log_prob_f32(sum, l, zact);
         w.item[p].H = H;
+        w.item[p].ls = l.ls;
         if (MODE == kTypesLogp && io.entropy) io.entropy[e] = H;
         if (MODE == kTypesLogp && io.lse) {
             io.lse[2 * e] = m;
@@ -1098,18 +1085,19 @@ __device__ __forceinline__ void types_grads(const WaveTile &w, const TypesIO &io
         const int64_t e = r0 * w.ns + p;
         float *x = w.zs + ri * w.a;
         const float2 g = w.row[ri];
-        float m, l2s, H = 0.f;
+        float m, inv_s, rest = 0.f, H = 0.f;
         if (MODE == kTypesLoss || MODE == kTypesPairs) {
-            m = w.item[p].m, l2s = w.item[p].l2s;
-            if (MODE == kTypesLoss) H = w.item[p].H;
+            m = w.item[p].m, inv_s = w.item[p].inv_s;
+            if (MODE == kTypesLoss) H = w.item[p].H, rest = w.item[p].ls;
         } else if (MODE == kTypesGradPairs) {
-            m = -INFINITY, l2s = 0.f;
-            if (g.x != 0.f) m = io.norm[e].x, l2s = io.norm[e].y;
+            m = -INFINITY, inv_s = 1.f;
+            if (g.x != 0.f) m = io.norm[e].x, inv_s = io.norm[e].y;
         } else {
-            m = io.in_lse[2 * e], l2s = io.in_lse[2 * e + 1] * kLog2e;
+            m = io.in_lse[2 * e], rest = io.in_lse[2 * e + 1];
+            inv_s = exp2_hw(-rest * kLog2e);
             if (g.y != 0.f) H = io.in_entropy[e];
         }
-        const RowCoef k = coef_of(m, m == -INFINITY ? 0.f : 1.f, l2s, H, g.x, g.y);
+        const RowCoef k = coef_of(m, m == -INFINITY, inv_s, rest, H, g.x, g.y);
         if (k.zero != 0.f) {
             for (int c = i0 + gl; c < i1; c += L) x[c] = 0.f;
             continue;
@@ -1686,7 +1674,7 @@ int preference_loss_launch(const harl_policy_head *head, const harl_preference_c
         if (const int rc = launch_types<kTypesDiff>(head, q, io, stream)) return rc;
     } else if (n_rows > 0) {
         const StatOut o{w.stat, nullptr, nullptr, nullptr};
-        if (const int rc = launch_wide_stats<kPartialLogp>(head, q, chunks, o, stream)) return rc;
+        if (const int rc = launch_wide_stats<kPartial>(head, q, chunks, o, stream)) return rc;
     }
     // a thread a row of an average pair
     const auto pairs = (int64_t)n_pairs * 256 < n_rows ? k_pairs<1024> : k_pairs<256>;
