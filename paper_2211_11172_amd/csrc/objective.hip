@@ -167,16 +167,29 @@ struct Sums {
 
 __device__ __forceinline__ float shift_of(float m) { return m == -INFINITY ? 0.f : m; }
 
+// FINE: u is not the entropy's sum but sum 2^y (d log2 e - y), d = z - m: what the products y = d log2 e were
+// rounded by and log2 e misses.  The difference of two log-probabilities summed over a track's rows needs it: bf16
+// logits are few values, whose roundings do not cancel (1e-8 a row).  log s is then ln s + ln 2 u / s.
+__device__ __forceinline__ float missed(float d, float y) { return fmaf(d, (float)kLog2eRest, fmaf(d, kLog2e, -y)); }
+
 // Moves the sums to a larger maximum (its shift ms = shift_of(m_new)).
+template <bool FINE = false>
 __device__ __forceinline__ void rescale(Sums &q, float m_new, float ms) {
-    const float d = (q.m - ms) * kLog2e, f = exp2_hw(d);
-    q.u = f * (q.u + q.s * fmaxf(d, -1e4f));
-    q.s *= f;
+    if (FINE) {
+        const float d = fmaxf(q.m - ms, -1e4f), y = d * kLog2e, f = q.m == -INFINITY ? 0.f : exp2_hw(y);
+        q.u = f * fmaf(q.s, missed(d, y), q.u);
+        q.s *= f;
+        if (q.m != q.m || m_new != m_new) q.s = __builtin_nanf("");
+    } else {
+        const float d = (q.m - ms) * kLog2e, f = exp2_hw(d);
+        q.u = f * (q.u + q.s * fmaxf(d, -1e4f));
+        q.s *= f;
+    }
     q.m = m_new;
 }
 
 // Adds NV vectors or single values to a lane's sums, with one change of the maximum.
-template <int NV, int N>
+template <bool FINE, int NV, int N>
 __device__ __forceinline__ void add_values(Sums &q, const float (&x)[NV][N]) {
     float gm = -INFINITY;
 #pragma unroll
@@ -184,22 +197,28 @@ __device__ __forceinline__ void add_values(Sums &q, const float (&x)[NV][N]) {
 #pragma unroll
         for (int i = 0; i < N; ++i) gm = max_nan(gm, x[j][i]);
     const float m = max_nan(q.m, gm), ms = shift_of(m);
-    rescale(q, m, ms);
+    rescale<FINE>(q, m, ms);
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const float y = fmaxf((x[j][i] - ms) * kLog2e, kYMin), e = exp2_hw(y);
-            q.s += e;
-            q.u = fmaf(e, y, q.u);
+            if (FINE) {
+                const float d = fmaxf(x[j][i] - ms, kYMin), y = d * kLog2e, e = exp2_hw(y);
+                q.s += e;
+                q.u = fmaf(e, missed(d, y), q.u);
+            } else {
+                const float y = fmaxf((x[j][i] - ms) * kLog2e, kYMin), e = exp2_hw(y);
+                q.s += e;
+                q.u = fmaf(e, y, q.u);
+            }
         }
 }
-template <int N, int NV>
+template <bool FINE, int N, int NV>
 __device__ __forceinline__ void add_vectors(Sums &q, const uint4 *raw) {
     float x[NV][N];
 #pragma unroll
     for (int j = 0; j < NV; ++j) unpack(raw[j], x[j]);
-    add_values<NV, N>(q, x);
+    add_values<FINE, NV, N>(q, x);
 }
 
 // Reductions over the first W lanes of a wave (W a power of two up to 64); the result in every lane.
@@ -217,10 +236,10 @@ __device__ __forceinline__ float lanes_reduce(float x, float none, Op op) {
     if constexpr (W > 32) x = op(x, dpp<0x143, 0xc>(x, none));  // row_bcast:31 into rows 2 and 3
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), W - 1));
 }
-template <int W>
+template <int W, bool FINE = false>
 __device__ __forceinline__ Sums lanes_join(Sums q) {
     const float m = lanes_reduce<W>(q.m, -INFINITY, [](float a, float b) { return max_nan(a, b); });
-    rescale(q, m, shift_of(m));
+    rescale<FINE>(q, m, shift_of(m));
     const auto add = [](float a, float b) { return a + b; };
     return Sums{m, lanes_reduce<W>(q.s, 0.f, add), lanes_reduce<W>(q.u, 0.f, add)};
 }
@@ -241,14 +260,14 @@ __device__ __forceinline__ double wave_sum(double x) {
 
 // The sums of a row from those of its TPR threads, in every thread.  `red` has 2 halves of TPR / 64
 // entries, used in turn, so that one barrier a row is enough.
-template <int TPR>
+template <int TPR, bool FINE = false>
 __device__ __forceinline__ Sums row_join(Sums q, Sums (*red)[16], int &half) {
-    q = lanes_join<64>(q);
+    q = lanes_join<64, FINE>(q);
     if constexpr (TPR > 64) {
         constexpr int W = TPR / 64;
         if (threadIdx.x % 64 == 0) red[half][threadIdx.x / 64] = q;
         __syncthreads();
-        q = lanes_join<W>(red[half][threadIdx.x % W]);
+        q = lanes_join<W, FINE>(red[half][threadIdx.x % W]);
         half ^= 1;
     }
     // NaN or +inf among the values: everything that follows is NaN
@@ -338,10 +357,10 @@ __device__ __forceinline__ void grad_vec(T *dz, int i0, const uint4 &raw, const 
 }
 
 // ---- statistics of (row, chunk) items: a chunk is `per` vectors, the first also has the row's edges ----
-enum Out : int { kPartial = 0, kLogp = 1 };
+enum Out : int { kPartial = 0, kLogp = 1, kPartialFine = 2 };
 
 struct StatOut {
-    Stat *stat;  // kPartial: [row][chunk] {m, s, u, z[action]}
+    Stat *stat;  // kPartial, kPartialFine: [row][chunk] {m, s, u, z[action]}
     float *logp, *entropy, *lse;
 };
 
@@ -358,6 +377,7 @@ __device__ __forceinline__ void put_logp(const StatOut &o, int64_t r, const Sums
 template <typename T, int TPR, int NV, int OUT>
 __global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void k_stats(Rows q, int chunks, int per, StatOut o) {
     constexpr int WG = TPR < kThreads ? kThreads : TPR, N = kVec<T>, G = NV < 4 ? NV : 4;
+    constexpr bool FINE = OUT == kPartialFine;
     __shared__ Sums red[2][16];
     int half = 0;
     const int t = threadIdx.x % TPR;
@@ -387,15 +407,15 @@ __global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void k_stats(Rows 
 #pragma unroll
                 for (int j = g; j < g + G; ++j)
                     if (TPR * (j + 1) > left && t + TPR * j >= left) raw[j] = all_excluded<T>();
-                add_vectors<N, G>(sum, raw + g);
+                add_vectors<FINE, N, G>(sum, raw + g);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
         if (c == 0 && parts.head + parts.tail > 0) {
             const float x[1][1] = {{ex}};
-            add_values<1, 1>(sum, x);
+            add_values<FINE, 1, 1>(sum, x);
         }
-        sum = row_join<TPR>(sum, red, half);
+        sum = row_join<TPR, FINE>(sum, red, half);
         if (t == 0) {
             if (OUT == kLogp) put_logp(o, r, sum, zact);
             else o.stat[it] = Stat{sum.m, sum.s, sum.u, zact};
@@ -404,6 +424,7 @@ __global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void k_stats(Rows 
 }
 
 // A row's sums from its chunks', by one thread in chunk order, eight loads in flight.
+template <bool FINE = false>
 __device__ __forceinline__ Sums join_chunks(const Stat *__restrict__ st, int chunks) {
     if (chunks == 1) return Sums{st[0].m, st[0].s, st[0].u};
     Sums q{-INFINITY, 0.f, 0.f};
@@ -415,11 +436,11 @@ __device__ __forceinline__ Sums join_chunks(const Stat *__restrict__ st, int chu
 #pragma unroll
         for (int j = 0; j < 8; ++j) m = max_nan(m, x[j].m);
         const float ms = shift_of(m);
-        rescale(q, m, ms);
+        rescale<FINE>(q, m, ms);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             Sums y{x[j].m, x[j].s, x[j].u};
-            rescale(y, m, ms);
+            rescale<FINE>(y, m, ms);
             if (c + j < chunks) {
                 q.s += y.s;
                 q.u += y.u;
@@ -528,14 +549,14 @@ __global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void k_loss(Rows q
         for (int j = 0; j < NV; ++j) {
             if (TPR * j >= full) continue;  // uniform
             if (TPR * (j + 1) > full && t + TPR * j >= full) raw[j] = all_excluded<T>();
-            add_vectors<N, 1>(sum, raw + j);
+            add_vectors<false, N, 1>(sum, raw + j);
             __builtin_amdgcn_sched_barrier(0);
         }
         for (int v = t + TPR * NV; v < full; v += TPR)  // what the registers do not hold
-            add_vectors<N, 1>(sum, reinterpret_cast<const uint4 *>(body) + v);
+            add_vectors<false, N, 1>(sum, reinterpret_cast<const uint4 *>(body) + v);
         if (parts.head + parts.tail > 0) {
             const float x[1][1] = {{ex}};
-            add_values<1, 1>(sum, x);
+            add_values<false, 1, 1>(sum, x);
         }
         sum = row_join<TPR>(sum, red, half);
         const LogSum l = log_sum_f32(sum);
@@ -665,8 +686,10 @@ __global__ __launch_bounds__(WG) void k_pairs(PairArgs a, const Stat *__restrict
                 const float w = a.weight ? a.weight[r] : 1.f;
                 if (w == 0.f) continue;
                 const float ref = a.logp_ref ? a.logp_ref[r] : 0.f;
-                const Sums q = join_chunks(stat + r * a.chunks, a.chunks);
-                d = (double)w * (log_prob(q, stat[r * a.chunks].zact) - (double)ref);
+                const Sums q = join_chunks<true>(stat + r * a.chunks, a.chunks);
+                const double ls = log((double)q.s) + kLn2d * (double)q.u / (double)q.s;
+                const double lp = q.s == 0.f ? 0.0 : ((double)stat[r * a.chunks].zact - (double)q.m) - ls;
+                d = (double)w * (lp - (double)ref);
                 if (fin) {
                     fin[r].m = q.s == 0.f ? -INFINITY : q.m;
                     fin[r].inv_s = 1.f / q.s;
@@ -1674,7 +1697,7 @@ int preference_loss_launch(const harl_policy_head *head, const harl_preference_c
         if (const int rc = launch_types<kTypesDiff>(head, q, io, stream)) return rc;
     } else if (n_rows > 0) {
         const StatOut o{w.stat, nullptr, nullptr, nullptr};
-        if (const int rc = launch_wide_stats<kPartial>(head, q, chunks, o, stream)) return rc;
+        if (const int rc = launch_wide_stats<kPartialFine>(head, q, chunks, o, stream)) return rc;
     }
     // a thread a row of an average pair
     const auto pairs = (int64_t)n_pairs * 256 < n_rows ? k_pairs<1024> : k_pairs<256>;
