@@ -1,0 +1,158 @@
+"""Policy objectives where their launches change shape: rows that a workgroup's registers do not hold, gradients
+beyond the caches, tracks longer than a workgroup's tiles, tracks of very unequal lengths.  Rows are drawn on the
+GPU; a sample of them goes through the fp64 oracle with the bars of tests/test_gpu_objective.py."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+
+from oracle import objective as obj
+from tests.gpu_util import log, require_gpu
+from tests.test_gpu_objective import CFG, E, Rows, SEGS_26, _bars, _close, _grad_bar, _top_p, check_pref, run_pref
+
+pytestmark = pytest.mark.gpu
+
+
+def _draw(dtype, M, a, pad, seed):
+    import torch
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    td = torch.bfloat16 if dtype == "bf16" else torch.float32
+    buf = torch.empty(M, a + pad, dtype=td, device="cuda")
+    for i in range(0, M, 256):
+        buf[i:i + 256] = (torch.randn(min(256, M - i), a + pad, generator=g, device="cuda") * 2).to(td)
+    f = lambda: torch.randn(M, generator=g, device="cuda")  # noqa: E731
+    return buf, torch.randint(0, a, (M, 1), generator=g, device="cuda", dtype=torch.int32), f
+
+
+@pytest.mark.parametrize("dtype,a,pad", [("f32", 66001, 3), ("f32", 65540, 0), ("bf16", 131080, 0), ("bf16", 139003, 2)])
+def test_rows_beyond_the_registers(dtype, a, pad):
+    """1,030 rows: a workgroup a row, whose last vectors are read twice; the loss of all rows is that of two calls
+    of half of them, which cut their rows into chunks."""
+    require_gpu()
+    import torch
+    from paper_2211_11172_amd import harl
+    M = 1030
+    log("policy loss: %s %d x %d" % (dtype, M, a))
+    buf, act, f = _draw(dtype, M, a, pad, a)
+    head, cfg = harl.policy_head(dtype, a), harl.policy_loss_config(**CFG)
+    ld = a + pad
+    lp = torch.empty(M, device="cuda")
+    wsb = max(harl.harl_policy_loss_workspace_size(head, M), harl.harl_policy_logp_workspace_size(head, M))
+    ws = torch.empty(wsb, dtype=torch.uint8, device="cuda")
+    harl.harl_policy_logp(head, buf, ld, M, act, lp, None, None, ws, wsb)
+    old, ref, adv = lp - 0.15 * torch.sign(f()), lp + 0.3 * f(), f()
+    w = torch.rand(M, device="cuda") / M
+    w[::5] = 0
+    dz, loss, new = torch.zeros_like(buf), torch.empty(4, device="cuda"), torch.empty(M, device="cuda")
+    harl.harl_policy_loss(head, cfg, buf, ld, M, act, old, ref, adv, w, dz, ld, new, loss, ws, wsb)
+    halves = torch.empty(2, 4, device="cuda")
+    for k in range(2):
+        s = slice(515 * k, 515 * (k + 1))
+        harl.harl_policy_loss(head, cfg, buf[s], ld, 515, act[s], old[s], ref[s], adv[s], w[s], None, 0, None, halves[k], ws, wsb)
+    torch.cuda.synchronize()
+    # the two ways sum a row in another order: a few steps of log s and of each term, relative to the terms' sizes
+    n = a / 64 + 100
+    scale = (w * (adv.abs() * 2 + 2 + 14)).sum().item()
+    assert (loss - halves.sum(0)).abs().max().item() <= 4 * E * n * scale
+    rows = [0, 1, 2, 5, 511, 1029]
+    z = buf[rows, :a].double().cpu().numpy()
+    acts = act[rows].cpu().numpy()
+    t = lambda x: x[rows].cpu().numpy()  # noqa: E731
+    c = {k: float(np.float32(v)) for k, v in CFG.items()}
+    O = obj.policy_loss(z, [0, a], acts, t(old), t(ref), t(adv), t(w), **c)
+    _, lp_e, _ = _bars(O["st"], [0, a])
+    on = t(w) != 0
+    lp_e = np.where(on, lp_e, 0.0)
+    _close(t(new), O["logp"], lp_e + E * np.abs(O["logp"]), "logp")
+    dg = np.abs(t(w)) * (np.abs(t(adv)) * O["ratio"] + c["w_kl"] * np.exp(t(ref) - O["logp"])) * lp_e + 2 * E * np.abs(O["g_logp"])
+    tol = _grad_bar(O["st"], [0, a], acts, O["g_logp"], O["g_ent"], dg, 2 * E * np.abs(O["g_ent"]), O["dlogits"], dtype, False)
+    _close(dz[rows, :a].double().cpu().numpy(), O["dlogits"], tol, "dlogits")
+    if pad:
+        assert (dz[:, a:] == 0).all()
+
+
+@pytest.mark.parametrize("dtype,M,a", [("bf16", 700, 60000), ("f32", 9000, 2000)])
+def test_gradients_beyond_the_caches(dtype, M, a):
+    """More than 64 MB of gradient: forward and backward, and the preference loss of long tracks."""
+    require_gpu()
+    import torch
+    from paper_2211_11172_amd import harl
+    log("logp and preference gradients: %s %d x %d" % (dtype, M, a))
+    buf, act, f = _draw(dtype, M, a, 0, M)
+    head = harl.policy_head(dtype, a)
+    lp, H, L = torch.empty(M, device="cuda"), torch.empty(M, 1, device="cuda"), torch.empty(M, 1, 2, device="cuda")
+    n = max(harl.harl_policy_logp_workspace_size(head, M), harl.harl_preference_loss_workspace_size(head, M, 2))
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    harl.harl_policy_logp(head, buf, a, M, act, lp, H, L, ws, n)
+    g, ge, dz = f(), f(), torch.zeros_like(buf)
+    g[3], ge[3] = 0, 0
+    harl.harl_policy_logp_grad(head, buf, a, M, act, L, H, g, ge, dz, a)
+    rows = [0, 3, 4, M // 2, M - 1]
+    z, acts = buf[rows].double().cpu().numpy(), act[rows].cpu().numpy()
+    st = obj.row_stats(z, [0, a], acts)
+    lse_e, lp_e, H_e = _bars(st, [0, a])
+    t = lambda x: x[rows].cpu().numpy()  # noqa: E731
+    _close(t(lp), st["logp"], lp_e + E * np.abs(st["logp"]), "logp")
+    _close(t(H), st["H"], H_e, "entropy")
+    _close(t(L)[:, :, 1], -np.log(_top_p(st, [0, a])), lse_e + E * np.log(a), "log-sum-exp")
+    gl, gh, zero = t(g).astype(np.float64), t(ge).astype(np.float64), np.zeros(5)
+    want = obj.logit_grad(st, [0, a], acts, gl, gh)
+    _close(dz[rows].double().cpu().numpy(), want, _grad_bar(st, [0, a], acts, gl, gh, zero, zero, want, dtype, True), "dlogits")
+    # preference: 2 pairs; the rows' gradients follow from the ratios that the call returns
+    ptr = torch.tensor([0, M // 3, M // 2, M // 2 + 5, M - 2], dtype=torch.int32, device="cuda")
+    ratio, loss = torch.empty(4, device="cuda"), torch.empty(4, device="cuda")
+    ref = lp + 0.2 * f()
+    dz.fill_(7.0)
+    harl.harl_preference_loss(head, harl.preference_config(0.1), buf, a, M, act, ref, None, ptr, 2, dz, a, ratio, loss, ws, n)
+    torch.cuda.synchronize()
+    R = ratio.double().cpu().numpy()
+    d = (lp.double() - ref.double()).cpu().numpy()
+    p = ptr.cpu().numpy()
+    want_R = np.array([d[p[q]:p[q + 1]].sum() for q in range(4)])
+    # lp and ref are fp32: half a step of |logp| <= 32 a row beside the rows' own bars
+    assert (np.abs(R - want_R) <= (lp_e.max() + 2 * 32 * E) * np.diff(p) + E * np.abs(R)).all()
+    h = float(np.float32(0.1)) * (R[0::2] - R[1::2])
+    gh = float(np.float32(0.1)) / 2 * -(1.0 / (1.0 + np.exp(h)))
+    assert (dz[M - 2:] == 7).all()
+    seq = np.searchsorted(p[1:], rows, side="right")
+    for k, r in enumerate(rows):
+        if r >= p[-1]:
+            continue
+        gl = np.array([gh[seq[k] // 2] * (1 if seq[k] % 2 == 0 else -1)])
+        one = {key: v[k:k + 1] for key, v in st.items()}
+        want = obj.logit_grad(one, [0, a], acts[k:k + 1], gl, np.zeros(1))
+        # R is rounded: h to 0.1 E |R| a track, the gradient to a quarter of 0.1 / 2 of that
+        dg = np.array([0.0125 * 0.1 * E * np.abs(R).max() * 4]) + 4 * E * np.abs(gl)
+        tol = _grad_bar(one, [0, a], acts[k:k + 1], gl, np.zeros(1), dg, np.zeros(1), want, dtype, False)
+        _close(dz[r:r + 1].double().cpu().numpy(), want, tol, "preference dlogits")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lens", [[0, 400] + [1, 2] * 39, [37, 1, 0, 0, 250, 251] + [3, 3] * 30, [2000, 3], [1, 1500, 700, 2]])
+def test_unequal_tracks_with_types(lens, dtype):
+    """One launch for short tracks, with one among them that its tiles do not hold; long tracks in three."""
+    require_gpu()
+    ptr = np.concatenate([[0], np.cumsum(lens)]).astype(np.int64)
+    for kw in (dict(), dict(off=3, pad=3), dict(in_place=True)):
+        R = Rows(dtype, int(ptr[-1]), SEGS_26, seed=len(lens), excl=0.1, **kw)
+        w = np.where(R.rng.random(R.M) < 0.2, 0.0, 1.0).astype(np.float32)
+        ref = (obj.row_stats(R.z, SEGS_26, R.acts)["logp"] + 0.2 * R.rng.standard_normal(R.M)).astype(np.float32)
+        cfg = dict(beta=0.2, smoothing=0.05)
+        check_pref(R, ref, w, ptr, cfg, run_pref(R, ref, w, ptr, cfg))
+
+
+def test_workspace_for_more_rows_serves_fewer():
+    require_gpu()
+    import torch
+    from paper_2211_11172_amd import harl
+    for segs in (SEGS_26, [0, 9001]):
+        R = Rows("bf16", 30, segs, seed=12)
+        n = harl.harl_preference_loss_workspace_size(R.head, 4000, 100)
+        ws = torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda")
+        ptr = np.array([0, 9, 14, 20, 30])
+        ratio, loss = R.f32(4), R.f32(4)
+        harl.harl_preference_loss(R.head, harl.preference_config(0.1), R.logits, R.ld, 30, R.d_acts, None, None,
+                                  R.dev(ptr.astype(np.int32)), 2, R.grad, R.ld_d, ratio, loss, ws, n)
+        torch.cuda.synchronize()
+        check_pref(R, None, None, ptr, dict(beta=0.1, smoothing=0.0), (loss.cpu().numpy(), ratio.cpu().numpy(), R.take_grad()))
