@@ -1387,6 +1387,13 @@ Rows rows_of(const harl_policy_head *h, const void *z, int64_t ld, int32_t M, co
 
 unsigned grid_for(int64_t items) { return (unsigned)std::min<int64_t>(std::max<int64_t>(items, 1), kMaxGrid); }
 
+// Which kernels take a head: several segments go by types, and so does one of few columns, where a wave a row
+// leaves lanes idle.  65,536 rows by rows / by types, us: the clipped loss of 24 columns 33 / 12, of 128 33 / 23, of
+// 256 43 / 53; log-probabilities and their gradient of 24 98 / 14, of 256 114 / 64, of 512 133 / 105; the preference
+// loss of 24 125 / 24, of 512 162 / 133.  (One column has no division by multiplication; it goes by rows.)
+constexpr int kTypesLossColumns = 128, kTypesColumns = 512;
+bool by_types(const harl_policy_head *h, int most) { return h->n_seg > 1 || (h->a > 1 && h->a <= most); }
+
 // ---- launch shapes of one-segment heads ----
 int vec_of(const harl_policy_head *h) { return h->dtype == HARL_BF16 ? 8 : 4; }
 
@@ -1560,15 +1567,15 @@ Ws ws_layout(const WsCounts &n, char *base) {
 
 // Rows in chunks: at most rows + kSplitItems items, and none in chunks from kSplitItems rows on.
 Ws logp_ws(const harl_policy_head *h, int64_t M, char *base) {
-    return ws_layout(WsCounts{h->n_seg == 1 ? std::min<int64_t>(M, kSplitItems) + kSplitItems : 0, 0, 0, 0, 0}, base);
+    return ws_layout(WsCounts{!by_types(h, kTypesColumns) ? std::min<int64_t>(M, kSplitItems) + kSplitItems : 0, 0, 0, 0, 0}, base);
 }
 Ws loss_ws(const harl_policy_head *h, int64_t M, char *base) {
-    return ws_layout(WsCounts{h->n_seg == 1 ? std::min<int64_t>(M, kSplitItems) + kSplitItems : 0, 0, 0, 0,
+    return ws_layout(WsCounts{!by_types(h, kTypesLossColumns) ? std::min<int64_t>(M, kSplitItems) + kSplitItems : 0, 0, 0, 0,
                               3 * std::min<int64_t>(M, kLossGrid)}, base);
 }
 Ws preference_ws(const harl_policy_head *h, int64_t rows, int64_t pairs, char *base) {
     const int64_t cut = std::min<int64_t>(kMaxChunks, std::max<int64_t>(1, ceil_div(h->a / vec_of(h), kPrefChunk)));
-    return ws_layout(h->n_seg == 1 ? WsCounts{rows * cut + kSplitItems, rows, 0, 0, 4 * pairs}
+    return ws_layout(!by_types(h, kTypesColumns) ? WsCounts{rows * cut + kSplitItems, rows, 0, 0, 4 * pairs}
                                    : WsCounts{0, 0, rows, rows * h->n_seg, 4 * pairs}, base);
 }
 
@@ -1586,7 +1593,7 @@ int policy_logp_launch(const harl_policy_head *head, const void *logits, int64_t
                        float *logp, float *entropy, float *lse, void *ws, hipStream_t stream) {
     const Ws w = logp_ws(head, M, static_cast<char *>(ws));
     const Rows q = rows_of(head, logits, ld, M, actions);
-    if (head->n_seg > 1) {
+    if (by_types(head, kTypesColumns)) {
         TypesIO io{};
         io.logp = logp;
         io.entropy = entropy;
@@ -1616,7 +1623,7 @@ int policy_logp_grad_launch(const harl_policy_head *head, const void *logits, in
                             const int32_t *actions, const float *lse, const float *entropy, const float *g_logp,
                             const float *g_entropy, void *dlogits, int64_t ld_d, hipStream_t stream) {
     const Rows q = rows_of(head, logits, ld, M, actions);
-    if (head->n_seg > 1) {
+    if (by_types(head, kTypesColumns)) {
         TypesIO io{};
         io.in_lse = lse;
         io.in_entropy = entropy;
@@ -1645,7 +1652,7 @@ int policy_loss_launch(const harl_policy_head *head, const harl_policy_loss_conf
     q.weight = weight;
     const LossArgs a{logp_old, logp_ref, adv, weight, cfg->clip_low, cfg->clip_high, cfg->w_kl, cfg->w_entropy, 1.f / (float)M};
     int64_t n_terms = 0;
-    if (head->n_seg > 1) {
+    if (by_types(head, kTypesLossColumns)) {
         TypesIO io{};
         io.loss = a;
         io.logp = logp;
@@ -1688,7 +1695,7 @@ int preference_loss_launch(const harl_policy_head *head, const harl_preference_c
     q.weight = weight;
     q.seq_ptr = seq_ptr;
     q.n_seq = 2 * n_pairs;
-    const bool grad = dlogits && n_rows > 0, types = head->n_seg > 1;
+    const bool grad = dlogits && n_rows > 0, types = by_types(head, kTypesColumns);
     const int chunks = !types && n_rows > 0 ? pref_chunks_for(head, n_rows) : 1;
     const PairArgs a{logp_ref, weight, seq_ptr, n_rows, chunks, n_pairs, cfg->beta, cfg->smoothing};
     if (n_rows > 0 && types) {
