@@ -8,7 +8,8 @@ import pytest
 
 from oracle import objective as obj
 from tests.gpu_util import log, require_gpu
-from tests.test_gpu_objective import CFG, E, Rows, SEGS_26, _bars, _close, _grad_bar, _top_p, check_pref, run_pref
+from tests.test_gpu_objective import (CFG, E, Rows, SEGS_26, _bars, _close, _grad_bar, _top_p, check_logp, check_loss,
+                                       check_pref, loss_inputs, run_logp, run_loss, run_pref)
 
 pytestmark = pytest.mark.gpu
 
@@ -72,7 +73,7 @@ def test_rows_beyond_the_registers(dtype, a, pad):
         assert (dz[:, a:] == 0).all()
 
 
-@pytest.mark.parametrize("dtype,M,a", [("bf16", 700, 60000), ("f32", 9000, 2000)])
+@pytest.mark.parametrize("dtype,M,a", [("bf16", 700, 60000), ("f32", 9000, 2000), ("bf16", 40000, 1003)])
 def test_gradients_beyond_the_caches(dtype, M, a):
     """More than 64 MB of gradient: forward and backward, and the preference loss of long tracks."""
     require_gpu()
@@ -156,3 +157,50 @@ def test_workspace_for_more_rows_serves_fewer():
                                   R.dev(ptr.astype(np.int32)), 2, R.grad, R.ld_d, ratio, loss, ws, n)
         torch.cuda.synchronize()
         check_pref(R, None, None, ptr, dict(beta=0.1, smoothing=0.0), (loss.cpu().numpy(), ratio.cpu().numpy(), R.take_grad()))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_widest_head(dtype):
+    """HARL_HEAD_MAX_COLUMNS columns: three rows in chunks, every call."""
+    require_gpu()
+    from paper_2211_11172_amd import harl
+    a = harl.HARL_HEAD_MAX_COLUMNS
+    for kw in (dict(), dict(off=1, pad=3)):
+        R = Rows(dtype, 3, [0, a], seed=31, **kw)
+        check_logp(R, run_logp(R))
+        inp = loss_inputs(R, CFG)
+        check_loss(R, inp, CFG, run_loss(R, inp, CFG))
+        ptr, cfg = [0, 2, 3], dict(beta=0.1, smoothing=0.0)
+        check_pref(R, None, None, ptr, cfg, run_pref(R, None, None, ptr, cfg))
+
+
+@pytest.mark.parametrize("segs", [SEGS_26, [0, 90], [0, 1300], [0, 20003]], ids=lambda s: "%dx%d" % (s[-1], len(s) - 1))
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gradient_in_the_place_of_the_logits(segs, dtype):
+    """harl_policy_logp_grad onto its own logits, aligned and not, gives what it gives elsewhere."""
+    require_gpu()
+    import torch
+    from paper_2211_11172_amd import harl
+    for kw in (dict(), dict(off=3, pad=1)):
+        got = []
+        for in_place in (False, True):
+            R = Rows(dtype, 21, segs, seed=77, excl=0.1, in_place=in_place, **kw)
+            lp, H, L = run_logp(R)
+            g = torch.linspace(-1, 1, 21, device="cuda")
+            g[10] = 0
+            harl.harl_policy_logp_grad(R.head, R.logits, R.ld, 21, R.d_acts, L, H, g, g * 0.1, R.grad, R.ld_d)
+            torch.cuda.synchronize()
+            got.append(R.take_grad())
+        np.testing.assert_array_equal(got[0], got[1])
+
+
+def test_many_pairs():
+    """More pairs than one launch takes at once."""
+    require_gpu()
+    rng = np.random.default_rng(8)
+    for dtype, segs in (("f32", SEGS_26), ("bf16", [0, 40]), ("f32", [0, 700])):
+        ptr = np.concatenate([[0], np.cumsum(rng.integers(0, 5, 2 * 1500))]).astype(np.int64)
+        R = Rows(dtype, int(ptr[-1]), segs, seed=9)
+        cfg = dict(beta=0.3, smoothing=0.1)
+        ref = (obj.row_stats(R.z, segs, R.acts)["logp"] + 0.4 * rng.standard_normal(R.M)).astype(np.float32)
+        check_pref(R, ref, None, ptr, cfg, run_pref(R, ref, None, ptr, cfg))
