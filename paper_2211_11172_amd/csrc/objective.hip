@@ -665,12 +665,13 @@ struct PairArgs {
 // Pair p's terms from its log ratios (written where `put`), and the gradient of the preferred track's.
 __device__ __forceinline__ double pair_terms(const PairArgs &a, int64_t p, const double (&R)[2], bool put, double *terms, float *ratio) {
     const double h = (double)a.beta * (R[0] - R[1]);
-    // -log sigmoid(h) = log(1 + e^-|h|) + max(-h, 0); d/dh of the loss = smoothing - sigmoid(-h)
+    // -log sigmoid(h) = log(1 + e^-|h|) + max(-h, 0), -log sigmoid(-h) the same of -h; d/dh of the loss = smoothing -
+    // sigmoid(-h).  Each part has a sum of its own: h = -inf gives inf and 0, where their difference h gives NaN.
     const double e = exp(-fabs(h));
     const double down = (h >= 0.0 ? e : 1.0) / (1.0 + e);
     if (put) {
-        const double lose = log1p(e) + (h < 0.0 ? -h : (h == h ? 0.0 : h));
-        terms[p * 4] = a.smoothing != 0.f ? lose + (double)a.smoothing * h : lose;
+        const double near = log1p(e), lose = near + (h < 0.0 ? -h : 0.0), win = near + (h > 0.0 ? h : 0.0);  // NaN: e is
+        terms[p * 4] = a.smoothing != 0.f ? (1.0 - (double)a.smoothing) * lose + (double)a.smoothing * win : lose;
         terms[p * 4 + 1] = lose;
         terms[p * 4 + 2] = h;
         terms[p * 4 + 3] = h > 0.0 ? 1.0 : 0.0;
