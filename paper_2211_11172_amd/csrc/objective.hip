@@ -69,9 +69,13 @@ struct LossArgs {
     float inv_m;
 };
 
+// The ratio of two probabilities ends at e^690 (a product with any advantage but 0 is infinite in fp32 long before), so
+// that an advantage of 0 gives 0 whatever the ratio is, and not 0 times infinity.
+constexpr double kTopLog = 690.0;
+
 // One row's terms of the clipped loss, weighted.
 __device__ __forceinline__ void loss_row(const LossArgs &a, int64_t r, float w, double logp, double H, double (&term)[3]) {
-    const double ratio = exp(logp - (double)a.logp_old[r]);
+    const double d = logp - (double)a.logp_old[r], ratio = exp(d > kTopLog ? kTopLog : d);
     const double adv = a.adv[r], lo = 1.0 - (double)a.clip_low, hi = 1.0 + (double)a.clip_high;
     const double s1 = ratio * adv, s2 = (ratio < lo ? lo : ratio > hi ? hi : ratio) * adv;
     double kl = 0.0;
@@ -480,26 +484,58 @@ struct LossOut {
     double *terms;  // [workgroup][3]: the sums of its rows' terms, in row order
 };
 
-// loss_row in fp32, evaluated by every wave of a row: in 64 bits it takes 100 registers beside the row's.
-// e^x - x - 1 near 0 comes from its series, where the difference would cancel.
+// loss_grad's terms of a log ratio beyond kLargeLog: e^89 is more than fp32 holds, 1e-4 e^89 is not, and 0 e^89 is 0.  The
+// weight goes into the terms first, and an exponential is the product of two.  (A branch for these rows costs the others
+// nothing that the timer shows; products in 64 bits for all rows took 0-8% more, 1.7% over 28 shapes.)
+constexpr float kLargeLog = 30.f;
+
+__device__ __forceinline__ void loss_grad_large(const LossArgs &a, float w, float d, float x, float adv, float &gl,
+                                                float &surrogate, float &kl, float &w_left) {
+    const auto times_exp = [](float v, float of, float &e) {  // v e^of, and e = e^of; an exponent of 166 is as good as infinite
+        const float y = of * kLog2e > 240.f ? 240.f : of * kLog2e, n = y > 120.f ? 120.f : 0.f;
+        const float e1 = exp2_hw(y - n), e2 = n > 0.f ? 0x1p120f : 1.f;
+        e = e1 * e2;
+        return (v * e1) * e2;
+    };
+    const float lo = 1.f - a.clip_low, hi = 1.f + a.clip_high, wa = fabsf(w);
+    float ratio, e, dk = 0.f;  // kl comes as of a small x
+    const float s1 = times_exp(adv * wa, d, ratio), s2 = (ratio < lo ? lo : ratio > hi ? hi : ratio) * (adv * wa);
+    const bool inside = ratio >= lo && ratio <= hi;
+    if (a.logp_ref) {
+        const float we = times_exp(wa, x, e);
+        kl = x > kLargeLog ? (x < INFINITY ? (we - wa) - x * wa : x) : kl * wa;
+        if (a.w_kl != 0.f) dk = a.w_kl * (wa - we);
+    }
+    w_left = copysignf(1.f, w);
+    surrogate = s2 < s1 ? s2 : s1;
+    gl = w_left * ((s2 < s1 && !inside ? 0.f : -s1) + dk);
+}
+
+// loss_row in fp32, evaluated by every wave of a row: in 64 bits it takes 100 registers beside the row's, and only the
+// logarithm, the log ratios and the products in 64 bits still 5% over 28 shapes (1-14% of each).
+// e^x - x - 1 near 0 comes from its series, where the difference would cancel.  surrogate and kl have yet to be
+// multiplied by w_left.
 __device__ __forceinline__ void loss_grad(const LossArgs &a, float w, float old, float ref, float adv, float logp, float &gl,
-                                          float &ge, float &surrogate, float &kl) {
-    const float ratio = exp2_hw((logp - old) * kLog2e);
+                                          float &ge, float &surrogate, float &kl, float &w_left) {
+    const float d = logp - old, x = a.logp_ref ? ref - logp : 0.f;
     const float lo = 1.f - a.clip_low, hi = 1.f + a.clip_high;
+    const float ratio = exp2_hw(d * kLog2e);
     const float s1 = ratio * adv, s2 = (ratio < lo ? lo : ratio > hi ? hi : ratio) * adv;
     const bool inside = ratio >= lo && ratio <= hi;
     const float ds = s2 < s1 && !inside ? 0.f : -s1;
     float dk = 0.f;
     kl = 0.f;
     if (a.logp_ref) {
-        const float x = ref - logp, e = exp2_hw(x * kLog2e);
+        const float e = exp2_hw(x * kLog2e);
         const float series = x * x * fmaf(x, fmaf(x, fmaf(x, fmaf(x, fmaf(x, 1.f / 5040.f, 1.f / 720.f), 1.f / 120.f), 1.f / 24.f), 1.f / 6.f), 0.5f);
-        kl = fabsf(x) < 0.25f ? series : x < INFINITY ? (e - 1.f) - x : x;
+        kl = fabsf(x) < 0.25f ? series : (e - 1.f) - x;
         if (a.w_kl != 0.f) dk = a.w_kl * (1.f - e);
     }
     surrogate = s2 < s1 ? s2 : s1;
     gl = w * (ds + dk);
     ge = -w * a.w_entropy;
+    w_left = w;
+    if (__builtin_expect(fmaxf(d, x) > kLargeLog, 0)) loss_grad_large(a, w, d, x, adv, gl, surrogate, kl, w_left);
 }
 
 // The whole row dz = 0, or (other alignment than the logits') an element at a time from memory.
@@ -533,8 +569,15 @@ __device__ __forceinline__ void grad_slices(const T *dz_body, int full, const ui
 // (a copy of 2 GB moves 4.9), 1,024 x 65,521 fp32 rows in 110 us (4.6 TB/s).  All loads of a row are issued at
 // once and its sums follow them in order; a workgroup of 16 waves holds 131,072 bf16 columns in 64 of its 128
 // registers a lane.  Row terms in fp64 and loads under masks took 255 registers and spilled (1,623 us).
+//
+// Waves a SIMD at least: as many as a row's registers leave.  The fewest columns need them all: 65,536 rows of 256 fp32
+// columns fill 8 waves of every SIMD four times (42 us; with 7 waves 45.5).
+template <typename T, int TPR, int NV>
+constexpr int kLossWaves = NV == 1 ? (sizeof(T) == 4 ? 8 : 7) : NV <= 4 ? (sizeof(T) == 4 ? 7 : TPR == 64 ? 6 : 5)
+                         : NV == 8 ? (sizeof(T) == 4 || TPR == 64 ? 5 : 4) : TPR == 1024 ? 4 : 3;
+
 template <typename T, int TPR, int NV, bool GRAD>
-__global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void k_loss(Rows q, LossArgs a, LossOut o) {
+__global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR, (kLossWaves<T, TPR, NV>)) void k_loss(Rows q, LossArgs a, LossOut o) {
     constexpr int WG = TPR < kThreads ? kThreads : TPR, N = kVec<T>;
     __shared__ Sums red[2][16];
     __shared__ double part[WG / TPR][3];
@@ -579,10 +622,10 @@ __global__ __launch_bounds__(TPR < kThreads ? kThreads : TPR) void k_loss(Rows q
         sum = row_join<TPR>(sum, red, half);
         const LogSum l = log_sum_f32(sum);
         const float logp = log_prob_f32(sum, l, zact), H = entropy_f32(sum, l);
-        float gl, ge, surrogate, kl;
-        loss_grad(a, w, old, ref, adv, logp, gl, ge, surrogate, kl);
-        acc[0] -= (double)w * (double)surrogate;
-        acc[1] += (double)w * (double)kl;
+        float gl, ge, surrogate, kl, w_left;
+        loss_grad(a, w, old, ref, adv, logp, gl, ge, surrogate, kl, w_left);
+        acc[0] -= (double)w_left * (double)surrogate;
+        acc[1] += (double)w_left * (double)kl;
         acc[2] += (double)w * (double)H;
         if (t == 0 && o.logp) o.logp[r] = logp;
         if (!GRAD) continue;
@@ -858,9 +901,9 @@ __global__ __launch_bounds__(kThreads) void k_grad(Rows q, int chunks, int per, 
                 const Sums s = join_wave(a.stat + (int64_t)r * a.stat_chunks, a.stat_chunks, zact);
                 const LogSum l = log_sum_f32(s);
                 const float H = entropy_f32(s, l), logp = log_prob_f32(s, l, zact);
-                float gl, ge, surrogate, kl;
+                float gl, ge, surrogate, kl, w_left;
                 loss_grad(a.loss, w, a.loss.logp_old[r], a.loss.logp_ref ? a.loss.logp_ref[r] : 0.f, a.loss.adv[r], logp, gl, ge,
-                          surrogate, kl);
+                          surrogate, kl, w_left);
                 k = coef_of(s.m, s.s == 0.f, l.inv_s, l.ls, H, gl, ge);
                 hot = grad_any(k, zact) + k.g;
             }
@@ -1261,10 +1304,10 @@ __global__ __launch_bounds__(kThreads, 5) void k_types(Rows q, TypesShape sh, Ty
             if (MODE == kTypesDiff) io.diff[r] = w == 0.f ? 0.0 : (double)w * (lp - (double)ref);
             if (MODE == kTypesLoss) {
                 if (w != 0.f) {
-                    float surrogate, kl;
-                    loss_grad(io.loss, w, old, ref, adv, (float)lp, g.x, g.y, surrogate, kl);
-                    acc[0] -= (double)w * (double)surrogate;
-                    acc[1] += (double)w * (double)kl;
+                    float surrogate, kl, w_left;
+                    loss_grad(io.loss, w, old, ref, adv, (float)lp, g.x, g.y, surrogate, kl, w_left);
+                    acc[0] -= (double)w_left * (double)surrogate;
+                    acc[1] += (double)w_left * (double)kl;
                     acc[2] += (double)w * H;
                 }
                 if (io.logp) io.logp[r] = w != 0.f ? (float)lp : 0.f;
