@@ -335,7 +335,9 @@ typedef struct {
  *   g_logp (1[i = action] - p) - g_H p (log p + H_s).
  *   d_dlogits [M][ld_d] of head->dtype out (rounded once, to nearest): the gradient; columns
  *            a .. ld_d-1 are left as they were.  It may be d_logits itself with ld_d == ld (the
- *            gradient replaces the logits); any other overlap is an error.
+ *            gradient replaces the logits), and with ld_d == ld its rows may lie between those of the
+ *            logits (one buffer's columns); any other overlap is an error, with ld_d != ld one of the
+ *            spans from the first row's first column to the last row's last.
  *   Sums are fp32 over a row's columns (a row's maximum subtracted) and fp64 over rows and segments.
  *   16-byte alignment of the first row and of ld lets the kernels move 16 bytes at a time
  *   throughout; other rows move 16 bytes at a time behind their first aligned column, and their

@@ -273,6 +273,17 @@ static int head_check(const std::string &who, const harl_policy_head *h) {
     return HARL_OK;
 }
 
+// Whether two sets of M rows of `width` bytes share a byte.  Rows of one stride: row i of the one meets row i + k of the
+// other where their starts are less than a row's width apart, and only two k bring them that near.  Rows of different
+// strides: their whole spans.
+static bool rows_meet(uintptr_t x, int64_t stride_x, uintptr_t y, int64_t stride_y, int64_t M, int64_t width) {
+    const int64_t span_x = (M - 1) * stride_x + width, span_y = (M - 1) * stride_y + width;
+    if (x >= y + (uintptr_t)span_y || y >= x + (uintptr_t)span_x) return false;
+    if (stride_x != stride_y) return true;
+    const int64_t apart = (int64_t)(y - x), near = (apart % stride_x + stride_x) % stride_x, k = (near - apart) / stride_x;
+    return (near < width && k > -M && k < M) || (stride_x - near < width && k - 1 > -M && k - 1 < M);
+}
+
 // Logits, actions and the optional gradient of M >= 1 rows.
 static int rows_check(const std::string &who, const harl_policy_head *h, const void *logits, int64_t ld, int32_t M,
                       const int32_t *actions, const void *dlogits, int64_t ld_d) {
@@ -285,8 +296,8 @@ static int rows_check(const std::string &who, const harl_policy_head *h, const v
     if (!aligned(dlogits, es)) return fail(HARL_E_INVALID_ARG, who + ": misaligned gradient");
     if (ld_d < h->a || ld_d > most) return fail(HARL_E_INVALID_ARG, who + ": need a <= ld_d (and rows that 2^56 elements hold)");
     if (dlogits == logits && ld_d == ld) return HARL_OK;
-    const uintptr_t z = reinterpret_cast<uintptr_t>(logits), d = reinterpret_cast<uintptr_t>(dlogits);
-    if (z < d + ((M - 1) * ld_d + h->a) * es && d < z + ((M - 1) * ld + h->a) * es)
+    const int64_t e = (int64_t)es;
+    if (rows_meet(reinterpret_cast<uintptr_t>(logits), ld * e, reinterpret_cast<uintptr_t>(dlogits), ld_d * e, M, h->a * e))
         return fail(HARL_E_INVALID_ARG, who + ": gradient and logits overlap without being the same rows");
     return HARL_OK;
 }

@@ -1,0 +1,101 @@
+"""Where the gradient's rows may lie beside those of the logits: the check on a host without a GPU, against every
+pair of rows, and the calls themselves."""
+from __future__ import annotations
+
+import ctypes
+
+import numpy as np
+import pytest
+
+from paper_2211_11172_amd import harl
+from tests.gpu_util import require_gpu
+
+A = 26
+BASE = 0x100000
+
+
+def _meet(off, ld, ld_d, M):
+    """Whether any row of A columns of the logits shares an element with one of the gradient, `off` elements on."""
+    z, d = np.arange(M) * ld, off + np.arange(M) * ld_d
+    return bool((np.abs(z[:, None] - d[None, :]) < A).any())
+
+
+def _loss(off, ld, ld_d, M, es):
+    """harl_policy_loss with a workspace too small: HARL_E_WORKSPACE comes behind the check of the rows."""
+    head, cfg = harl.policy_head("f32" if es == 4 else "bf16", A), harl.policy_loss_config()
+    return harl.load().harl_policy_loss(ctypes.byref(head), ctypes.byref(cfg), BASE, ld, M, 0x1000, 0x1000, None, 0x1000, None,
+                                        BASE + off * es, ld_d, None, 0x3000, 0x5000, 0, None)
+
+
+@pytest.mark.parametrize("es", [2, 4])
+@pytest.mark.parametrize("M", [1, 2, 3, 7])
+def test_rows_of_one_stride(M, es):
+    """Refused exactly where a row meets a row, or is the same row (allowed)."""
+    for ld in (26, 27, 40, 52, 53, 80):
+        for off in list(range(-4 * ld - 30, 4 * ld + 31)) + [-9 * ld, 9 * ld]:
+            want = harl.HARL_E_INVALID_ARG if off != 0 and _meet(off, ld, ld, M) else harl.HARL_E_WORKSPACE
+            assert _loss(off, ld, ld, M, es) == want, (off, ld)
+            if want == harl.HARL_E_INVALID_ARG:
+                assert "overlap" in harl.harl_last_error()
+
+
+def test_rows_of_two_strides():
+    """Spans that meet are refused, rows that meet always."""
+    for M in (1, 2, 5):
+        for ld, ld_d in ((52, 60), (60, 52), (26, 90)):
+            for off in range(-5 * 90 - 30, 5 * 90 + 31, 1):
+                spans = off < (M - 1) * ld + A and -off < (M - 1) * ld_d + A
+                got = _loss(off, ld, ld_d, M, 4)
+                assert got == (harl.HARL_E_INVALID_ARG if spans else harl.HARL_E_WORKSPACE)
+                assert spans or not _meet(off, ld, ld_d, M)
+
+
+def test_rows_beyond_32_bits():
+    """2^31 - 1 rows, 64 MB apart."""
+    M, ld = 2 ** 31 - 1, 1 << 24
+    for off, want in ((32, harl.HARL_E_WORKSPACE), (25, harl.HARL_E_INVALID_ARG), (ld * (M - 1) + 25, harl.HARL_E_INVALID_ARG),
+                      (ld * (M - 1) + 26, harl.HARL_E_WORKSPACE), (ld * 1000 - 26, harl.HARL_E_WORKSPACE), (ld * 1000 - 25, harl.HARL_E_INVALID_ARG)):
+        assert _loss(off, ld, ld, M, 4) == want, off
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("segs,M", [([0, 17, 20, 23, 26], 70), ([0, 300], 70), ([0, 9008], 20), ([0, 4208], 1030)],
+                         ids=lambda v: str(v) if isinstance(v, int) else "%dx%d" % (v[-1], len(v) - 1))
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gradient_between_the_logits(segs, M, dtype):
+    """Logits in the left half of a buffer's columns, the gradient in the right half: what it is in a buffer of its
+    own, and the logits stay."""
+    require_gpu()
+    import torch
+    a, half = segs[-1], -(-segs[-1] // 16) * 16
+    td = torch.bfloat16 if dtype == "bf16" else torch.float32
+    g = torch.Generator(device="cuda")
+    g.manual_seed(a)
+    z = (torch.randn(M, a, generator=g, device="cuda") * 2).to(td)
+    acts = torch.stack([torch.randint(lo, hi, (M,), generator=g, device="cuda", dtype=torch.int32) for lo, hi in zip(segs, segs[1:])], 1).contiguous()
+    adv, ptr = torch.randn(M, generator=g, device="cuda"), torch.tensor([0, 3, M // 2, M // 2 + 4, M], dtype=torch.int32, device="cuda")
+    head = harl.policy_head(dtype, a, segs)
+    n = max(harl.harl_policy_loss_workspace_size(head, M), harl.harl_policy_logp_workspace_size(head, M),
+            harl.harl_preference_loss_workspace_size(head, M, 2))
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    out = []
+    for between in (False, True):
+        both = torch.full((M, 2 * half), 7.0, dtype=td, device="cuda")
+        both[:, :a] = z
+        logits = both[:, :a]
+        grad = (both if between else torch.full_like(both, 7.0))[:, half:half + a]
+        ld = 2 * half
+        lp, H, L = torch.empty(M, device="cuda"), torch.empty(M, len(segs) - 1, device="cuda"), torch.empty(M, len(segs) - 1, 2, device="cuda")
+        harl.harl_policy_logp(head, logits, ld, M, acts, lp, H, L, ws, n)
+        got = [lp]
+        harl.harl_policy_logp_grad(head, logits, ld, M, acts, L, H, adv, adv, grad, ld)
+        got.append(grad.clone())
+        harl.harl_policy_loss(head, harl.policy_loss_config(w_entropy=0.01), logits, ld, M, acts, lp, None, adv, None, grad, ld, None, None, ws, n)
+        got.append(grad.clone())
+        harl.harl_preference_loss(head, harl.preference_config(), logits, ld, M, acts, None, None, ptr, 2, grad, ld, None, None, ws, n)
+        got.append(grad.clone())
+        torch.cuda.synchronize()
+        assert torch.equal(both[:, :a], z) and (both[:, a:half] == 7).all() and (both[:, half + a:] == 7).all()
+        out.append(got)
+    for x, y in zip(*out):
+        assert torch.equal(x, y)
