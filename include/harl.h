@@ -343,7 +343,8 @@ typedef struct {
  *   throughout; other rows move 16 bytes at a time behind their first aligned column, and their
  *   gradient does where d_dlogits has the same alignment.
  * M >= 0 (M == 0 is a no-op).  Arrays other than logits and gradient are 4-byte aligned; d_ws is
- * 256-byte aligned, its contents on entry do not matter.
+ * 256-byte aligned, its contents on entry do not matter.  But for the gradient in the place of the
+ * logits no output, nor d_ws, overlaps an input or another output (caller's precondition).
  */
 
 /* Bytes of device workspace harl_policy_logp needs for M rows. */
@@ -392,7 +393,7 @@ size_t harl_policy_loss_workspace_size(const harl_policy_head *head, int32_t M);
  *   d_logp_old, d_adv [M] fp32; d_logp_ref [M] fp32, or NULL (no KL term; w_kl must be 0).
  *   d_weight  [M] fp32, or NULL (1/M each).  A row of weight 0 is padding: none of its other values is
  *             read, it adds nothing to any sum, its d_logp is 0 and its gradient row is 0.
- *   d_dlogits out, or NULL; d_logp [M] fp32 out, or NULL.
+ *   d_dlogits out, or NULL; d_logp [M] fp32 out, or NULL; it may not overlap the rows' inputs.
  *   d_loss    [4] fp32 out, or NULL: the loss, and the weighted sums of -min(..), of the KL term
  *             without w_kl (0 without d_logp_ref) and of the entropies.
  * An excluded action that was chosen has ratio 0 and an infinite KL term (NaN where logp_ref is

@@ -367,6 +367,10 @@ int harl_policy_loss(const harl_policy_head *head, const harl_policy_loss_config
     if (cfg->w_kl != 0.f && !d_logp_ref) return fail(HARL_E_INVALID_ARG, "harl_policy_loss: w_kl needs logp_ref");
     if ((d_logp && !aligned(d_logp, 4)) || (d_loss && !aligned(d_loss, 4)))
         return fail(HARL_E_INVALID_ARG, "harl_policy_loss: misaligned output");
+    if (d_logp)  // written by one workgroup while others still read the row's values
+        for (const float *in : {d_logp_old, d_logp_ref, d_adv, d_weight})
+            if (in && rows_meet(reinterpret_cast<uintptr_t>(in), 4, reinterpret_cast<uintptr_t>(d_logp), 4, M, 4))
+                return fail(HARL_E_INVALID_ARG, "harl_policy_loss: logp overlaps one of the rows' inputs");
     if (const int rc = ws_check(who, d_ws, ws_bytes, harl::objective_loss_ws_bytes(head, M))) return rc;
     return harl::policy_loss_launch(head, cfg, d_logits, ld, M, d_actions, d_logp_old, d_logp_ref, d_adv, d_weight,
                                     d_dlogits, ld_d, d_logp, d_loss, d_ws, static_cast<hipStream_t>(stream));

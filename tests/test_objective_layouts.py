@@ -58,6 +58,20 @@ def test_rows_beyond_32_bits():
         assert _loss(off, ld, ld, M, 4) == want, off
 
 
+def test_logp_is_no_input():
+    """harl_policy_loss writes a row's log-probability while other workgroups read its inputs: each overlap is refused."""
+    head, cfg, M = harl.policy_head("f32", A), harl.policy_loss_config(), 9
+
+    def call(logp, old=0x1000, ref=0x2000, adv=0x3000, w=0x4000):
+        return harl.load().harl_policy_loss(ctypes.byref(head), ctypes.byref(cfg), BASE, A, M, 0x8000, old, ref, adv, w, None, 0, logp,
+                                            0x9000, 0xA000, 0, None)
+    for at in (0x1000, 0x2000, 0x3000, 0x4000):
+        for off in range(-4 * M - 8, 4 * M + 12, 4):
+            assert call(at + off) == (harl.HARL_E_INVALID_ARG if abs(off) < 4 * M else harl.HARL_E_WORKSPACE)
+    assert call(0x2000, ref=None) == harl.HARL_E_WORKSPACE and call(0x4000, w=None) == harl.HARL_E_WORKSPACE
+    assert call(None) == harl.HARL_E_WORKSPACE
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("segs,M", [([0, 17, 20, 23, 26], 70), ([0, 300], 70), ([0, 9008], 20), ([0, 4208], 1030)],
                          ids=lambda v: str(v) if isinstance(v, int) else "%dx%d" % (v[-1], len(v) - 1))
