@@ -325,10 +325,11 @@ typedef struct {
 /*
  * Common to the calls below.
  *   d_logits [M][ld] of head->dtype, aligned to its element (ld >= a; columns a .. ld-1 are not
- *            read).  A logit of -inf is an excluded action: probability 0, gradient 0.  A segment of
- *            nothing but -inf is empty: it adds 0 to log-probability and entropy and has gradient 0.
- *            The log-probability of an excluded action in a segment that is not empty is -inf.  NaN
- *            and +inf make their segment's results NaN.
+ *            read).  A logit of -inf is an excluded action: probability 0, and gradient 0 unless it
+ *            was chosen (then the formula's g_logp).  A segment of nothing but -inf is empty: it adds
+ *            0 to log-probability and entropy and has gradient 0.  The log-probability of an excluded
+ *            action in a segment that is not empty is -inf.  NaN and +inf make their segment's results
+ *            NaN.
  *   d_actions [M][n_seg] int32: row-global indices, each in its segment; others are clamped into it.
  *   Per row, over its segments s: lse_s = log sum exp(z), logp = sum_s (z[action_s] - lse_s),
  *   H_s = -sum p log p.  The gradient of g_logp logp + g_H sum_s H_s at a logit is
@@ -339,6 +340,9 @@ typedef struct {
  *            logits (one buffer's columns); any other overlap is an error, with ld_d != ld one of the
  *            spans from the first row's first column to the last row's last.
  *   Sums are fp32 over a row's columns (a row's maximum subtracted) and fp64 over rows and segments.
+ *   What follows from a row's sums (logarithm, log-probability, entropy, and in the clipped loss the
+ *   ratio, the KL term and their derivatives) is fp32, each rounded a few times at its own size; a
+ *   track's log ratio is fp64 from the sums on.
  *   16-byte alignment of the first row and of ld lets the kernels move 16 bytes at a time
  *   throughout; other rows move 16 bytes at a time behind their first aligned column, and their
  *   gradient does where d_dlogits has the same alignment.
@@ -367,7 +371,7 @@ int harl_policy_logp(const harl_policy_head *head, const void *d_logits, int64_t
  *   d_lse [M][n_seg][2], d_entropy [M][n_seg]: harl_policy_logp's outputs for the same logits;
  *             d_entropy may be NULL where d_g_entropy is.
  *   d_g_logp  [M] fp32; d_g_entropy [M] fp32 or NULL.
- * Rows whose gradients are 0 are set to 0 and their logits are not read.
+ * Rows whose gradients are 0 are set to 0 whatever their logits hold.
  */
 int harl_policy_logp_grad(const harl_policy_head *head, const void *d_logits, int64_t ld, int32_t M,
                           const int32_t *d_actions, const float *d_lse, const float *d_entropy,
@@ -391,13 +395,15 @@ size_t harl_policy_loss_workspace_size(const harl_policy_head *head, int32_t M);
  * min passes the gradient to the unclipped term on equality, clip inside its closed range (as in
  * harl_ppo_update, whose surrogate and entropy terms this gives for weights 1/M).
  *   d_logp_old, d_adv [M] fp32; d_logp_ref [M] fp32, or NULL (no KL term; w_kl must be 0).
- *   d_weight  [M] fp32, or NULL (1/M each).  A row of weight 0 is padding: none of its other values is
- *             read, it adds nothing to any sum, its d_logp is 0 and its gradient row is 0.
+ *   d_weight  [M] fp32, or NULL (1/M each).  A row of weight 0 is padding: none of its other values
+ *             counts (they may be read, and may hold anything), it adds nothing to any sum, its d_logp
+ *             is 0 and its gradient row is 0.
  *   d_dlogits out, or NULL; d_logp [M] fp32 out, or NULL; it may not overlap the rows' inputs.
  *   d_loss    [4] fp32 out, or NULL: the loss, and the weighted sums of -min(..), of the KL term
  *             without w_kl (0 without d_logp_ref) and of the entropies.
  * An excluded action that was chosen has ratio 0 and an infinite KL term (NaN where logp_ref is
- * -inf too).  Deterministic.
+ * -inf too); with w_kl > 0 its row's gradient is not finite.  A row of advantage 0 adds nothing to the
+ * surrogate and its gradient whatever its ratio is (unless that is NaN).  Deterministic.
  */
 int harl_policy_loss(const harl_policy_head *head, const harl_policy_loss_config *cfg,
                      const void *d_logits, int64_t ld, int32_t M, const int32_t *d_actions,
@@ -427,6 +433,9 @@ size_t harl_preference_loss_workspace_size(const harl_policy_head *head, int32_t
  *              as it was.
  *   d_dlogits  out, or NULL; d_ratio [2 n_pairs] fp32 out, or NULL: R_q.
  *   d_loss     [4] fp32 out, or NULL: the loss, and the means of -log sigmoid(h), of h and of [h > 0].
+ * An excluded action that was chosen makes its track's R -inf: the loss is +inf where that track is the
+ * preferred one, or with smoothing > 0; with one in both tracks there is no margin, and the loss and
+ * the pair's gradient are NaN.
  * n_pairs == 0 is a no-op; n_rows == 0 is not.  Deterministic.
  */
 int harl_preference_loss(const harl_policy_head *head, const harl_preference_config *cfg,

@@ -6,9 +6,9 @@ term to a reference policy (the estimator e^x - x - 1, x = logp_ref - logp, whic
 the policy's own samples and never negative), and the preference loss of paired log ratios of
 Rafailov et al., "Direct Preference Optimization" (NeurIPS'23), with label smoothing.  Conventions:
 
-  - a logit of -inf is an excluded action (probability 0, gradient 0); a segment of nothing but -inf
-    adds 0 to log-probability and entropy and has gradient 0;
-  - a row of weight 0 is padding: none of its values is read, its gradient is 0;
+  - a logit of -inf is an excluded action (probability 0, gradient 0 unless it was chosen); a segment of
+    nothing but -inf adds 0 to log-probability and entropy and has gradient 0;
+  - a row of weight 0 is padding: none of its values counts, its gradient is 0;
   - min passes the gradient to the unclipped term on equality, clip inside its closed range.
 
 Only tests/ uses this module.

@@ -37,7 +37,7 @@ struct Rows {
     int64_t ld;
     int M, a, n_seg;
     const int32_t *act;
-    const float *weight;     // rows of weight 0 are skipped, or null
+    const float *weight;     // rows of weight 0 count for nothing, or null
     const int32_t *seq_ptr;  // only rows of [seq_ptr[0], seq_ptr[n_seq]) count, or null
     int n_seq;
     int32_t off[HARL_SELECT_MAX_SEGMENTS + 1];
@@ -485,8 +485,8 @@ struct LossOut {
 };
 
 // loss_grad's terms of a log ratio beyond kLargeLog: e^89 is more than fp32 holds, 1e-4 e^89 is not, and 0 e^89 is 0.  The
-// weight goes into the terms first, and an exponential is the product of two.  (A branch for these rows costs the others
-// nothing that the timer shows; products in 64 bits for all rows took 0-8% more, 1.7% over 28 shapes.)
+// weight goes into the terms first, and an exponential is the product of two.  (The branch costs the other rows 0.1% over
+// 28 shapes; products in 64 bits for all rows, without it, took up to 8% more, 1.7% over all.)
 constexpr float kLargeLog = 30.f;
 
 __device__ __forceinline__ void loss_grad_large(const LossArgs &a, float w, float d, float x, float adv, float &gl,
@@ -512,7 +512,7 @@ __device__ __forceinline__ void loss_grad_large(const LossArgs &a, float w, floa
 }
 
 // loss_row in fp32, evaluated by every wave of a row: in 64 bits it takes 100 registers beside the row's, and only the
-// logarithm, the log ratios and the products in 64 bits still 5% over 28 shapes (1-14% of each).
+// logarithm, the log ratios and the products in 64 bits still 5% over 28 shapes (0-14% of each).
 // e^x - x - 1 near 0 comes from its series, where the difference would cancel.  surrogate and kl have yet to be
 // multiplied by w_left.
 __device__ __forceinline__ void loss_grad(const LossArgs &a, float w, float old, float ref, float adv, float logp, float &gl,
@@ -571,7 +571,7 @@ __device__ __forceinline__ void grad_slices(const T *dz_body, int full, const ui
 // registers a lane.  Row terms in fp64 and loads under masks took 255 registers and spilled (1,623 us).
 //
 // Waves a SIMD at least: as many as a row's registers leave.  The fewest columns need them all: 65,536 rows of 256 fp32
-// columns fill 8 waves of every SIMD four times (42 us; with 7 waves 45.5).
+// columns fill 8 waves of every SIMD four times (40 us; with 7 waves 45.5).
 template <typename T, int TPR, int NV>
 constexpr int kLossWaves = NV == 1 ? (sizeof(T) == 4 ? 8 : 7) : NV <= 4 ? (sizeof(T) == 4 ? 7 : TPR == 64 ? 6 : 5)
                          : NV == 8 ? (sizeof(T) == 4 || TPR == 64 ? 5 : 4) : TPR == 1024 ? 4 : 3;
@@ -781,6 +781,7 @@ __global__ __launch_bounds__(WG) void k_pairs(PairArgs a, const Stat *__restrict
     }
 }
 
+// By one workgroup: of 3,000 pairs' preference loss 1.5 of 23 us, of a million pairs' 0.35 of 2.3 ms.
 __device__ __forceinline__ void pairs_sum(const double *__restrict__ terms, int n_pairs, float *__restrict__ loss) {
     double s[4];
     sum_terms<4>(terms, n_pairs, s);
@@ -939,9 +940,11 @@ __global__ __launch_bounds__(kThreads) void k_grad(Rows q, int chunks, int per, 
 // Heads of several segments, up to 4,096 columns.  A wave owns up to 64 consecutive rows, staged in LDS
 // as fp32; `lanes` lanes share a (row, segment) item.  Everything a row needs stays in its wave, so there
 // are no barriers between the steps: stage, sums of every item, a lane a row for the objective, gradients
-// of every item in place, write back.  Bound by instructions where rows are many (8,192 x 1,034 fp32: 23 us, 13
-// at a copy's rate) and by the chain of the steps where they are few (4,096 x 26: 8 us, of which the sums take
-// 0.9, the rows' scalars 0.5, the gradients 0.8 and the arguments and first loads 2).
+// of every item in place, write back.  Rows of weight 0 are staged with the others; their gradient is 0.  Bound by
+// vector instructions and the waits between the steps where rows are many (8,192 x 1,034 fp32: 23 us, 13 at a copy's
+// rate; the vector units issue 60% of the time, LDS 30%, and a wave waits for 55% of its own) and by the chain of the
+// steps where they are few (4,096 x 26: 8 us, of which the sums take 0.9, the rows' scalars 0.5, the gradients 0.8 and
+// the arguments and first loads 2).
 // ------------------------------------------------------------------------------------------------
 enum TypesMode : int { kTypesLogp, kTypesDiff, kTypesLoss, kTypesGradLse, kTypesGradPairs, kTypesPairs };
 
@@ -1436,9 +1439,19 @@ Rows rows_of(const harl_policy_head *h, const void *z, int64_t ld, int32_t M, co
 unsigned grid_for(int64_t items) { return (unsigned)std::min<int64_t>(std::max<int64_t>(items, 1), kMaxGrid); }
 
 // Which kernels take a head: several segments go by types, and so does one of few columns, where a wave a row
-// leaves lanes idle.  65,536 rows by rows / by types, us: the clipped loss of 24 columns 33 / 12, of 128 33 / 23, of
-// 256 43 / 53; log-probabilities and their gradient of 24 98 / 14, of 256 114 / 64, of 512 133 / 105; the preference
-// loss of 24 125 / 24, of 512 162 / 133.  (One column has no division by multiplication; it goes by rows.)
+// leaves lanes idle.  65,536 rows by rows / by types, us:
+//                            24 columns  128      192      256      384      512      700
+//   clipped loss       fp32  35 / 12   36 / 24  40 / 41  42 / 54  51 / 70  56 / 81
+//                      bf16  41 / 12   41 / 22  41 / 32  42 / 42  46 / 54  48 / 65
+//   log-probabilities  fp32  56 / 12   59 / 27  64 / 46  69 / 64  79 / 85  90 / 106
+//   and gradient       bf16  71 / 12   73 / 22  73 / 35  74 / 45  79 / 58  83 / 73  96 / 107
+//   preference loss    fp32  64 / 19   70 / 36  73 / 55  77 / 74  83 / 96  97 / 118
+//                      bf16  79 / 19   84 / 30  86 / 44  86 / 56  88 / 68  91 / 83  104 / 120
+// bf16 rows cross at 1.3 to 2 times the columns of fp32 ones, so that one number of columns suits one type: fp32 rows of
+// 257 to 512 columns lose up to 21% to it, bf16 rows of 129 to 255 in the clipped loss up to 28%.  Rows with columns
+// between them are staged an element at a time and cross earlier (log-probabilities and gradient, fp32 192 columns
+// 73 / 67, 256 76 / 85, bf16 256 81 / 71, 512 91 / 124).
+// (One column has no division by multiplication; it goes by rows.)
 constexpr int kTypesLossColumns = 128, kTypesColumns = 512;
 bool by_types(const harl_policy_head *h, int most) { return h->n_seg > 1 || (h->a > 1 && h->a <= most); }
 
@@ -1451,7 +1464,10 @@ constexpr int kLossGrid = 8192;    // workgroups of k_loss: its terms
 constexpr int kPrefChunk = 2048;   // vectors of a preference row's chunk at most
 
 // Chunks of a row: rows that leave the machine idle are cut until there are about kSplitItems items, none of
-// fewer than 512 vectors (two a thread).
+// fewer than 512 vectors (two a thread).  The clipped loss then reads its logits twice.  Rows cut / whole in k_loss, us:
+// 131,072 bf16 columns, 16 rows 16 / 23, 64 17 / 26, 128 26 / 28, 256 49 / 36, 512 86 / 67, 1,000 176 / 128; 60,000, 128
+// rows 17 / 17, 1,000 85 / 69; 20,011 fp32 columns, 16 rows 12 / 10, 256 18 / 14, 1,000 58 / 44: from some 150 rows on
+// the cut costs that loss more than it gives, up to 47% (65,521 fp32 columns, 1,000 rows 168 / 115).
 int chunks_for(const harl_policy_head *h, int32_t M) {
     const int64_t vecs = h->a / vec_of(h);
     return (int)std::max<int64_t>(1, std::min<int64_t>({ceil_div(kSplitItems, M), (int64_t)kMaxChunks, vecs / 512}));
@@ -1755,7 +1771,9 @@ int preference_loss_launch(const harl_policy_head *head, const harl_preference_c
     if (n_rows > 0 && types) {
         // short tracks, and not more pairs than the machine takes at once: one launch in the place of three (256
         // pairs of 1 to 20 rows of 26 columns 20.9 -> 12.7 us; but 3,000 of them 30 -> 41 us, 30 of up to 100 rows
-        // 16.6 -> 20.6)
+        // 16.6 -> 20.6).  The tracks' lengths lie on the device: the rule sees their average, and where one pair holds
+        // nearly all rows one workgroup does nearly all the work (60,416 rows of 26 columns in 1,024 pairs 8.3 ms, in
+        // three launches 0.12, and evenly dealt 24 and 23 us; 7,424 rows in 256 pairs 1.0 ms and 27 us, 12 and 18).
         const TypesShape s = types_shape(head, n_rows, ceil_div(n_rows, 2 * (int64_t)n_pairs));  // twice the average pair
         if (n_pairs <= 1024 && (int64_t)n_rows * head->a <= (int64_t)n_pairs * 1536) {
             const size_t lds = 4 * (size_t)s.bytes;
